@@ -237,6 +237,103 @@ int gspn_scan_bwd(const void* dy, const void* x, const void* w, const void* lam,
                   int64_t group_h, int64_t group_w, uint32_t flags, int algo,
                   void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Linear attention with a decay for each head: the one-dimensional relative of
+ * the scan, over tokens (a map's raster, or any sequence).
+ *
+ *   S_t = exp(a_t) S_{t-1} + k_t v_t^T        S: Dk x Dv, fp32, S_{-1} = initial state
+ *   o_t = scale q_t S_t
+ *
+ * for every sequence and value head h, which uses query/key head h / (H / Hk)
+ * (H a multiple of Hk).  a is the log of the decay: one number for each head, or
+ * with GSPN_LINATTN_DECAY_PER_TOKEN one for each token and head.  a <= 0 is what
+ * a decay is; -inf empties the state in front of the token; positive values grow
+ * the state and are taken as they are.
+ *
+ * Layouts: q, k (B, T, Hk, Dk) and v (B, T, H, Dv) with the last axis dense and
+ * any non-negative strides on the others (`strides`: batch row, token and head of
+ * q, then of k, then of v, in elements, a host array; NULL: contiguous), so that
+ * slices of one projection need no copy.  log_decay (H) or (B, T, H), o, the
+ * output gradients and all gradients contiguous.  States (n_seq, H, Dk, Dv) are fp32
+ * whatever `dtype` is.  1 <= Dk, Dv <= 128, any T (0 too: the final state is the
+ * initial one).
+ *
+ * Sequences: without cu_seqlens B = n_seq sequences of T tokens.  With it (device,
+ * n_seq + 1 numbers that start at 0 and do not fall) B = 1 and sequence n is
+ * tokens cu_seqlens[n] .. cu_seqlens[n + 1] - 1 of the packed axis; empty ones are
+ * allowed.  Tokens behind the last sequence belong to none: their outputs
+ * and gradients are 0.  Positions outside [0, T] are taken as the nearest inside.
+ *
+ * Arithmetic: sums, decays and states in fp32 (exponents in 64 bits).  With bf16
+ * tensors the state is rounded to bf16 where it meets q, and products of q and k
+ * where they meet v (as operands of matrix instructions); what is added to a
+ * state is not rounded.  A non-finite value of a token reaches the outputs of the
+ * up to 64 tokens of its chunk, earlier ones of the same sequence too.
+ * Results repeat bit for bit.
+ * ------------------------------------------------------------------------- */
+enum { GSPN_LINATTN_DECAY_PER_TOKEN = 1u };
+
+size_t gspn_linattn_fwd_workspace_bytes(int64_t n_seq, int64_t B, int64_t T, int64_t H, int64_t Hk, int64_t Dk,
+                                        int64_t Dv, int packed, gspn_dtype dtype, uint32_t flags);
+size_t gspn_linattn_bwd_workspace_bytes(int64_t n_seq, int64_t B, int64_t T, int64_t H, int64_t Hk, int64_t Dk,
+                                        int64_t Dv, int packed, gspn_dtype dtype, uint32_t flags);
+
+/* Forward.  initial_state may be NULL (zero); final_state may be NULL (not
+ * wanted).  o and final_state are fully overwritten. */
+int gspn_linattn_fwd(const void* q, const void* k, const void* v, const void* log_decay,
+                     const float* initial_state, const int32_t* cu_seqlens, void* o, float* final_state,
+                     int64_t n_seq, int64_t B, int64_t T, int64_t H, int64_t Hk, int64_t Dk, int64_t Dv,
+                     const int64_t* strides, gspn_dtype dtype, uint32_t flags, float scale, void* workspace,
+                     size_t workspace_bytes, void* stream);
+
+/* Gradients of <dout, o> + <dfinal_state, final_state>, fully overwritten:
+ * dq, dk (B, T, Hk, Dk) summed over the value heads of each, dv, dlog_decay
+ * shaped like log_decay, dinitial_state (NULL: not wanted).  dfinal_state may be
+ * NULL (zero).  Nothing of the forward call is needed. */
+int gspn_linattn_bwd(const void* dout, const void* q, const void* k, const void* v, const void* log_decay,
+                     const float* initial_state, const float* dfinal_state, const int32_t* cu_seqlens, void* dq,
+                     void* dk, void* dv, void* dlog_decay, float* dinitial_state, int64_t n_seq, int64_t B,
+                     int64_t T, int64_t H, int64_t Hk, int64_t Dk, int64_t Dv, const int64_t* strides,
+                     gspn_dtype dtype, uint32_t flags, float scale, void* workspace, size_t workspace_bytes,
+                     void* stream);
+
+/* One token for each of B running sequences: state is updated in place, o
+ * (B, H, Dv).  q, k (B, Hk, Dk), v (B, H, Dv); strides: batch row and head of
+ * each.  log_decay (H), or (B, H) with GSPN_LINATTN_DECAY_PER_TOKEN.  state
+ * (n_slots, H, Dk, Dv), 16-byte aligned; row b uses slot slots[b] (device), or b
+ * where slots is NULL.  A slot outside [0, n_slots) leaves the row out: its output
+ * is 0.  Two rows with the same slot race. */
+int gspn_linattn_step(const void* q, const void* k, const void* v, const void* log_decay, float* state,
+                      const int32_t* slots, void* o, int64_t n_slots, int64_t B, int64_t H, int64_t Hk, int64_t Dk,
+                      int64_t Dv, const int64_t* strides, gspn_dtype dtype, uint32_t flags, float scale,
+                      void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Group norm with an activation, channels last: x (B, L, C) contiguous (L is the
+ * product of the map's sides, 1 for tokens on their own), G groups of C / G
+ * neighbouring channels, C <= 8192.
+ *
+ *   xh = (x - mean) rstd over the L x C/G values of a group, rstd = 1 / sqrt(var + eps)
+ *   y  = act(xh * weight + bias)
+ *
+ * weight and bias (C), element type `dtype`, may be NULL (ones, zeros).  The
+ * forward also writes mean and rstd (B, G), fp32, which the backward takes.
+ * Statistics and sums are fp32, taken around a value of the group.
+ * dweight and dbias may be NULL (not wanted).
+ * ------------------------------------------------------------------------- */
+enum { GSPN_ACT_NONE = 0, GSPN_ACT_SILU = 1, GSPN_ACT_GELU = 2 }; /* gelu: z/2 (1 + erf(z / sqrt 2)) */
+
+size_t gspn_group_norm_fwd_workspace_bytes(int64_t B, int64_t L, int64_t C, int64_t G, gspn_dtype dtype);
+size_t gspn_group_norm_bwd_workspace_bytes(int64_t B, int64_t L, int64_t C, int64_t G, gspn_dtype dtype);
+
+int gspn_group_norm_fwd(const void* x, const void* weight, const void* bias, void* y, float* mean, float* rstd,
+                        int64_t B, int64_t L, int64_t C, int64_t G, float eps, int act, gspn_dtype dtype,
+                        void* workspace, size_t workspace_bytes, void* stream);
+int gspn_group_norm_bwd(const void* dy, const void* x, const void* weight, const void* bias, const float* mean,
+                        const float* rstd, void* dx, void* dweight, void* dbias, int64_t B, int64_t L, int64_t C,
+                        int64_t G, int act, gspn_dtype dtype, void* workspace, size_t workspace_bytes,
+                        void* stream);
+
 /*
  * Plain device-to-device copy of `bytes` bytes (src and dst 16-byte aligned,
  * not overlapping).  Not part of the scan: it is the reference kernel of known

@@ -1,0 +1,137 @@
+// Launch interface of the linear-attention kernels (gspn_linattn_*.hip).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace gspn {
+namespace la {
+
+// How the sequences are cut into pieces (find_piece).
+struct Geom {
+  const int32_t* cu;  // packed: N + 1 positions on the device; null: N sequences of T tokens
+  int N, T;           // packed: T is the length of the packed axis
+  int L, P;           // tokens of a piece (a multiple of the chunk); pieces of a batched sequence
+  int pieces;         // piece indexes
+  int H, Hk, Dk, Dv;  // value heads, query/key heads, head sizes
+};
+
+// A token tensor: strides in elements of batch row, token and head, the last
+// axis dense; vec: every row starts on 16 bytes and is whole 16-byte vectors.
+struct Rows {
+  const void* p;
+  int64_t sb, st, sh;
+  int vec;
+};
+
+struct FwdArgs {
+  Geom g;
+  Rows q, k, v;
+  const void* a;          // log decays, (H) or (B, T, H)
+  int per_token;
+  float scale;
+  const float* s0;        // initial states (N, H, Dk, Dv), or null
+  float* sf;              // final states, or null
+  const float* start;     // start states of pieces that are not their sequence's first (register order)
+  void* o;                // (B, T, H, Dv)
+  int ovec;               // o's rows can be written four values at a time
+  void* stream;
+};
+hipError_t linattn_fwd_f32(const FwdArgs& a);
+hipError_t linattn_fwd_bf16(const FwdArgs& a);
+
+// Walks the state alone.  x runs along the registers, y along the lanes:
+//   S <- e^{G_C} S + sum_t f_t x_t y_t^T
+// forward: f_t = e^{G_C - G_t}; reverse (chunks from the last to the first):
+// f_t = scale e^{G_t}.
+struct StateArgs {
+  Geom g;
+  Rows x, y;
+  int x_shared, y_shared;  // the tensor has Hk heads
+  int Dx, Dy;              // sizes of the two sides
+  const void* a;
+  int per_token;
+  float scale;
+  int reverse;
+  // mode 0: pieces that are not their sequence's last (reverse: first), from a zero
+  // state: the state at the piece's end to `local`, its decay to `gtot`.
+  // mode 1: every piece from its start state (s0 or `local`): the state before
+  // each chunk, in the element type, to `chunks`.
+  int mode;
+  float* local;            // pieces x H register-order states
+  float* gtot;             // pieces x H
+  const float* s0;         // (N, H, Dk, Dv), or null
+  int sx, sy;              // s0's strides along x and y
+  void* chunks;            // pieces x (L / C) x H states
+  void* stream;
+};
+hipError_t linattn_state_f32(const StateArgs& a);
+hipError_t linattn_state_bf16(const StateArgs& a);
+
+// Pieces' own states -> their start states (reverse: end states), in place.
+struct JoinArgs {
+  Geom g;
+  float* local;
+  const float* gtot;
+  const float* s0;         // (N, H, Dk, Dv), or null
+  int Dx, Dy, sx, sy;
+  int reverse;
+  void* stream;
+};
+hipError_t linattn_join(const JoinArgs& a);
+
+struct BwdArgs {
+  Geom g;
+  Rows q, k, v, dout;
+  const void* a;
+  int per_token;
+  float scale;
+  const float* dsf;        // gradient of the final states, or null
+  float* ds0;              // gradient of the initial states, or null
+  const float* end;        // end-state gradients of pieces that are not their sequence's last
+  const void* chunks;      // state before each chunk (x = v, y = k)
+  void *dq, *dk, *dv;      // dq, dk: (B, T, Hk, Dk) when H == Hk, else null
+  int dkvec, dvvec;        // their rows can be written four values at a time
+  float *dq32, *dk32;      // (B, T, H, Dk) when H != Hk
+  void* da;                // per_token: (B, T, H)
+  float* da_piece;         // else: pieces x H sums
+  void* stream;
+};
+hipError_t linattn_bwd_f32(const BwdArgs& a);
+hipError_t linattn_bwd_bf16(const BwdArgs& a);
+
+// dq, dk of shared heads: sums over the value heads of each; dlog_decay (H): sums over the pieces.
+struct ReduceArgs {
+  int64_t tokens;
+  int H, Hk, Dk, dtype;
+  const float *dq32, *dk32;
+  void *dq, *dk;
+  const float* da_piece;   // null when per token
+  void* da;
+  int pieces;
+  void* stream;
+};
+hipError_t linattn_reduce(const ReduceArgs& a);
+
+struct StepArgs {
+  Rows q, k, v;            // st unused
+  const void* a;
+  int per_row;             // log decays (B, H), else (H)
+  float scale;
+  float* state;            // (slots, H, Dk, Dv)
+  const int32_t* slot;     // (B) or null
+  int64_t slots;
+  void* o;                 // (B, H, Dv)
+  int64_t B;
+  int H, Hk, Dk, Dv, dtype;
+  void* stream;
+};
+hipError_t linattn_step(const StepArgs& a);
+
+// register-order size of a state, in elements (sides padded to 64 or 128)
+inline int pad_dim(int d) { return d <= 64 ? 64 : 128; }
+inline int chunk_len(int dtype) { return dtype == 0 ? 32 : 64; }
+constexpr int kMaxDim = 128;
+
+}  // namespace la
+}  // namespace gspn

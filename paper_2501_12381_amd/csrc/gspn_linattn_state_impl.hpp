@@ -1,0 +1,94 @@
+// Linear attention: walks of the state alone (StateArgs): a piece's own state, for
+// the join of a cut sequence's pieces, and the states before each chunk, which
+// the backward reads.
+//
+// Bound by its bytes: x and y in, and in mode 1 a state of each chunk out.  The
+// chunks' states are written in the element type and in the order in which the
+// backward's products take them as operands (16 or 32 bytes a lane, one run of the
+// wave's 64 lanes each): it would round them to that type all the same.
+#pragma once
+
+#include "gspn_linattn_fwd_impl.hpp"
+
+namespace gspn {
+namespace la {
+
+template <typename T, int XP, int YP> __global__ void __launch_bounds__(2 * YP, 2) linattn_state_kernel(StateArgs A) {
+  constexpr int C = Elem<T>::kChunk, NT = 2 * YP;
+  constexpr int XS = XP + Elem<T>::kPad, YS = YP + Elem<T>::kPad;
+  __shared__ __align__(16) T sx[C * XS], sy[C * YS];
+  __shared__ Decays<C> dec;
+
+  const Geom& g = A.g;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, h = lane >> 5, l = lane & 31;
+  const int head = blockIdx.x % g.H, pi = blockIdx.x / g.H;
+  const Piece pc = find_piece(g, pi);
+  if (pc.len < 0 || pc.seq >= g.N) return;
+  if (A.mode == 0 && (A.reverse ? pc.first : pc.last)) return;  // nobody reads its state
+  const int hk = head / (g.H / g.Hk), yc = 32 * wave + l;
+  const int64_t slot = (int64_t)pi * g.H + head;
+  f32x16 S[XP / 32];
+  if (A.mode == 0) {
+#pragma unroll
+    for (int m = 0; m < XP / 32; ++m) S[m] = f32x16{};
+  } else if (pc.first) {
+    state_read<XP>(S, A.s0 ? A.s0 + ((int64_t)pc.seq * g.H + head) * A.Dx * A.Dy : nullptr, A.Dx, A.Dy, A.sx, A.sy,
+                   yc, h);
+  } else {
+    state_read_regs<XP>(S, A.local + slot * (XP * YP), wave, lane);
+  }
+  const T *x = head_rows<T>(A.x, pc, A.x_shared ? hk : head), *y = head_rows<T>(A.y, pc, A.y_shared ? hk : head);
+  const T* a = reinterpret_cast<const T*>(A.a) + head +
+               (A.per_token ? (pc.batch * g.T + pc.t0) * (int64_t)g.H : (int64_t)0);
+  const int64_t at = A.per_token ? g.H : 0;
+
+  Stage<T, XP, NT> rx;
+  Stage<T, YP, NT> ry;
+  double ra = 0.0, all = 0.0;
+  const auto load = [&](int t) {
+    const int rows = pc.len - t;
+    rx.load(x + t * A.x.st, A.x.st, rows, A.Dx, A.x.vec, tid);
+    ry.load(y + t * A.y.st, A.y.st, rows, A.Dy, A.y.vec, tid);
+    if (wave == 0 && lane < C) ra = load_decay(a + t * at, at, lane, rows);
+  };
+  const int n = (pc.len + C - 1) / C;
+  T* chunks = reinterpret_cast<T*>(A.chunks);
+  const float* f = A.reverse ? dec.qf : dec.kf;
+  if (n > 0) load((A.reverse ? n - 1 : 0) * C);
+  for (int i = 0; i < n; ++i) {
+    const int c = A.reverse ? n - 1 - i : i;
+    rx.store(sx, tid);
+    ry.store(sy, tid);
+    if (wave == 0) all += chunk_decays(dec, ra, A.scale, lane);
+    lds_barrier();
+    if (i + 1 < n) load((A.reverse ? c - 1 : c + 1) * C);
+    if (A.mode == 1) {
+      T* out = chunks + (((int64_t)pi * (g.L / C) + c) * g.H + head) * (XP * YP) + (wave * (XP / 16) * 64 + lane) * 8;
+#pragma unroll
+      for (int kk = 0; kk < XP / 16; ++kk) {
+        const auto fr = acc_frag<T>(S[kk >> 1], kk & 1);
+        *reinterpret_cast<typename Elem<T>::Frag*>(out + kk * 512) = fr;
+      }
+    }
+    state_add<T, XP>(S, sx, XS, sy, YS, 32 * wave, f, dec.tot, lane);
+    lds_barrier();
+  }
+  if (A.mode == 0) {
+    state_write_regs<XP>(S, A.local + slot * (XP * YP), wave, lane);
+    if (tid == 0) A.gtot[slot] = exp2_wide(all);
+  }
+}
+
+template <typename T> hipError_t linattn_state_t(const StateArgs& a) {
+  const dim3 grid((unsigned)((int64_t)a.g.pieces * a.g.H));
+  const hipStream_t st = (hipStream_t)a.stream;
+  const bool xw = a.Dx > 64, yw = a.Dy > 64;
+  if (xw && yw) hipLaunchKernelGGL((linattn_state_kernel<T, 128, 128>), grid, dim3(256), 0, st, a);
+  else if (xw) hipLaunchKernelGGL((linattn_state_kernel<T, 128, 64>), grid, dim3(128), 0, st, a);
+  else if (yw) hipLaunchKernelGGL((linattn_state_kernel<T, 64, 128>), grid, dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((linattn_state_kernel<T, 64, 64>), grid, dim3(128), 0, st, a);
+  return hipGetLastError();
+}
+
+}  // namespace la
+}  // namespace gspn

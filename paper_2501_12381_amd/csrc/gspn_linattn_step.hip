@@ -1,0 +1,183 @@
+// Linear attention: one token for each running sequence, and the small kernels
+// around the walks of long ones (the join of pieces, sums over shared heads).
+#include "gspn_linattn_common.hpp"
+
+namespace gspn {
+namespace la {
+namespace {
+
+// ---------------------------------------------------------------------------
+// single tokens: S <- e^a S + k v^T, o = scale q S
+// ---------------------------------------------------------------------------
+// Bound by the state's bytes, read and written once (8 of its 8 + 2/D bytes an
+// element).  One workgroup a state: a thread owns V neighbouring columns of
+// every 256 / (columns / V)'th row and has up to kBatch rows in flight; the sum
+// over the rows is joined through LDS.
+constexpr int kBatch = 8;
+
+template <typename T, int V> __global__ void __launch_bounds__(256) linattn_step_kernel(StepArgs A, int cshift) {
+  __shared__ float sq[kMaxDim], sk[kMaxDim];
+  __shared__ __align__(16) float so[256 * V];
+  const int tid = threadIdx.x;
+  const int64_t b = blockIdx.x / A.H;
+  const int head = blockIdx.x % A.H, hk = head / (A.H / A.Hk);
+  const int64_t slot = A.slot ? (int64_t)A.slot[b] : b;
+  T* o = reinterpret_cast<T*>(A.o) + (b * A.H + head) * A.Dv;
+  if (slot < 0 || slot >= A.slots) {  // an empty row
+    for (int i = tid; i < A.Dv; i += 256) o[i] = from_f<T>(0.f);
+    return;
+  }
+  const T *q = reinterpret_cast<const T*>(A.q.p) + b * A.q.sb + hk * A.q.sh,
+          *k = reinterpret_cast<const T*>(A.k.p) + b * A.k.sb + hk * A.k.sh,
+          *v = reinterpret_cast<const T*>(A.v.p) + b * A.v.sb + head * A.v.sh;
+  if (tid < A.Dk) {
+    sq[tid] = to_f(q[tid]) * A.scale;
+    sk[tid] = to_f(k[tid]);
+  }
+  const double la2 = (double)to_f(reinterpret_cast<const T*>(A.a)[A.per_row ? b * A.H + head : head]) *
+                     1.4426950408889634;
+  const float decay = exp2_wide(la2 < -150.0 ? -150.0 : la2);
+  const int cols = 1 << cshift, c = (tid & (cols - 1)) * V, r0 = tid >> cshift, rstep = 256 >> cshift;
+  const bool on = c < A.Dv;
+  float x[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) x[j] = on ? to_f(v[c + j]) : 0.f;
+  float* S = A.state + ((int64_t)slot * A.H + head) * A.Dk * A.Dv + c;
+  float acc[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) acc[j] = 0.f;
+  __syncthreads();
+  if (on) {
+    for (int r = r0; r < A.Dk; r += kBatch * rstep) {
+      float s[kBatch][V];
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i)
+        if (r + i * rstep < A.Dk) ldv<V>(S + (r + i * rstep) * A.Dv, s[i]);
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        const int row = r + i * rstep;
+        if (row < A.Dk) {
+#pragma unroll
+          for (int j = 0; j < V; ++j) {
+            s[i][j] = __builtin_fmaf(decay, s[i][j], sk[row] * x[j]);
+            acc[j] = __builtin_fmaf(sq[row], s[i][j], acc[j]);
+          }
+          if constexpr (V == 4)
+            *reinterpret_cast<float4*>(S + row * A.Dv) = make_float4(s[i][0], s[i][1], s[i][2], s[i][3]);
+          else
+            S[row * A.Dv] = s[i][0];
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < V; ++j) so[(r0 * cols * V) + (tid & (cols - 1)) * V + j] = acc[j];
+  __syncthreads();
+  if (tid < A.Dv) {
+    float t = 0.f;
+    for (int i = 0; i < rstep; ++i) t += so[i * cols * V + tid];
+    o[tid] = from_f<T>(t);
+  }
+}
+
+template <typename T> hipError_t step_t(const StepArgs& a) {
+  const dim3 grid((unsigned)(a.B * a.H));
+  const bool v4 = a.Dv % 4 == 0;
+  int cshift = 0;
+  while ((1 << cshift) * (v4 ? 4 : 1) < a.Dv) ++cshift;
+  if (v4) hipLaunchKernelGGL((linattn_step_kernel<T, 4>), grid, dim3(256), 0, (hipStream_t)a.stream, a, cshift);
+  else hipLaunchKernelGGL((linattn_step_kernel<T, 1>), grid, dim3(256), 0, (hipStream_t)a.stream, a, cshift);
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------------------
+// join of a sequence's pieces: running = gtot running + local, in register order
+// ---------------------------------------------------------------------------
+__global__ void __launch_bounds__(256) linattn_join_kernel(JoinArgs A, int XP, int YP) {
+  const Geom& g = A.g;
+  const int parts = XP * YP / 256, nh = blockIdx.x / parts, head = nh % g.H, n = nh / g.H;
+  int first, last;  // piece indexes
+  if (g.cu) {
+    const auto at = [&](int i) { return i == 0 ? 0 : max(0, min(g.T, (int)g.cu[i])); };
+    const int s = at(n), e = max(s, at(n + 1));
+    first = s / g.L + n;
+    last = max(s / g.L, (e - 1) / g.L) + n;
+  } else {
+    first = n * g.P;
+    last = first + g.P - 1;
+  }
+  if (first == last) return;
+  const int e = (blockIdx.x % parts) * 256 + threadIdx.x;  // register order: wave (y / 32), tile (x / 32), register, lane
+  const int lane = e & 63, r = (e >> 6) & 15, m = (e >> 10) % (XP / 32), w = (e >> 10) / (XP / 32);
+  const int x = 32 * m + acc_row(r, lane >> 5), y = 32 * w + (lane & 31);
+  const int64_t size = (int64_t)XP * YP;
+  float run = A.s0 && x < A.Dx && y < A.Dy
+                  ? A.s0[((int64_t)n * g.H + head) * A.Dx * A.Dy + x * A.sx + y * A.sy] : 0.f;
+  const int step = A.reverse ? -1 : 1, from = A.reverse ? last : first, to = A.reverse ? first : last;
+  float next = A.local[((int64_t)from * g.H + head) * size + e];
+  for (int i = from; i != to; i += step) {
+    run = __builtin_fmaf(A.gtot[(int64_t)i * g.H + head], run, next);
+    float* p = A.local + ((int64_t)(i + step) * g.H + head) * size + e;
+    if (i + step != to) next = *p;
+    *p = run;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// sums over the value heads of a query/key head, and over the pieces
+// ---------------------------------------------------------------------------
+template <typename T> __global__ void __launch_bounds__(256) linattn_share_kernel(ReduceArgs A) {
+  const int64_t n = A.tokens * A.Hk * A.Dk;
+  const int group = A.H / A.Hk;
+  const float* in = blockIdx.y ? A.dk32 : A.dq32;
+  T* out = reinterpret_cast<T*>(blockIdx.y ? A.dk : A.dq);
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    const int64_t th = i / A.Dk;  // token and query/key head
+    const int d = (int)(i - th * A.Dk);
+    const float* p = in + th * group * A.Dk + d;
+    float t = p[0];
+    for (int j = 1; j < group; ++j) t += p[(int64_t)j * A.Dk];
+    out[i] = from_f<T>(t);
+  }
+}
+
+template <typename T> __global__ void __launch_bounds__(256) linattn_decay_kernel(ReduceArgs A) {
+  __shared__ double s[256];
+  const int head = blockIdx.x, tid = threadIdx.x;
+  double t = 0.0;
+  for (int i = tid; i < A.pieces; i += 256) t += (double)A.da_piece[(int64_t)i * A.H + head];
+  s[tid] = t;
+  __syncthreads();
+  for (int k = 128; k > 0; k >>= 1) {
+    if (tid < k) s[tid] += s[tid + k];
+    __syncthreads();
+  }
+  if (tid == 0) reinterpret_cast<T*>(A.da)[head] = from_f<T>((float)s[0]);
+}
+
+template <typename T> hipError_t reduce_t(const ReduceArgs& a) {
+  const hipStream_t st = (hipStream_t)a.stream;
+  if (a.dq32 && a.tokens > 0) {
+    const int64_t n = a.tokens * a.Hk * a.Dk;
+    const unsigned blocks = (unsigned)(n < 2048 * 256 ? (n + 255) / 256 : 2048);
+    hipLaunchKernelGGL(linattn_share_kernel<T>, dim3(blocks, 2), dim3(256), 0, st, a);
+  }
+  if (a.da_piece) hipLaunchKernelGGL(linattn_decay_kernel<T>, dim3(a.H), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t linattn_step(const StepArgs& a) { return a.dtype == 0 ? step_t<float>(a) : step_t<bf16>(a); }
+
+hipError_t linattn_join(const JoinArgs& a) {
+  const int XP = pad_dim(a.Dx), YP = pad_dim(a.Dy);
+  hipLaunchKernelGGL(linattn_join_kernel, dim3((unsigned)((int64_t)(XP * YP / 256) * a.g.N * a.g.H)), dim3(256), 0,
+                     (hipStream_t)a.stream, a, XP, YP);
+  return hipGetLastError();
+}
+
+hipError_t linattn_reduce(const ReduceArgs& a) { return a.dtype == 0 ? reduce_t<float>(a) : reduce_t<bf16>(a); }
+
+}  // namespace la
+}  // namespace gspn

@@ -1,0 +1,476 @@
+// C ABI of linear attention and group norm: argument checking, workspace layout
+// and launches.  Host code only.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+
+#include "../../include/gspn.h"
+#include "gspn_groupnorm.hpp"
+#include "gspn_linattn.hpp"
+
+namespace {
+
+using namespace gspn;
+
+size_t round256(size_t v) { return (v + 255) / 256 * 256; }
+size_t esize(int dtype) { return dtype == GSPN_F32 ? 4 : 2; }
+
+bool mul_ok(int64_t a, int64_t b, int64_t* out) {
+  if (a != 0 && b > INT64_MAX / a) return false;
+  *out = a * b;
+  return true;
+}
+
+// bytes [lo, hi) of a tensor
+struct Span {
+  uintptr_t lo, hi;
+};
+Span span(const void* p, int64_t elements, size_t es) {
+  return {(uintptr_t)p, (uintptr_t)p + (p ? (size_t)elements * es : 0)};
+}
+bool overlap(const Span& a, const Span& b) { return a.lo < b.hi && b.lo < a.hi; }
+template <int I, int O> int check_spans(const Span (&in)[I], const Span (&out)[O]) {
+  for (int i = 0; i < O; ++i) {
+    for (int j = 0; j < I; ++j)
+      if (overlap(out[i], in[j])) return GSPN_ERR_ALIAS;
+    for (int j = i + 1; j < O; ++j)
+      if (overlap(out[i], out[j])) return GSPN_ERR_ALIAS;
+  }
+  return GSPN_OK;
+}
+bool aligned(const void* p, size_t a) { return (uintptr_t)p % a == 0; }
+
+// ---------------------------------------------------------------------------
+// linear attention
+// ---------------------------------------------------------------------------
+struct Lin {
+  int64_t B, T, N;
+  int H, Hk, Dk, Dv, dtype;
+  uint32_t flags;
+  bool packed;
+  la::Geom g;
+  int KP, VP, C;
+};
+
+// Sequences are cut where their heads alone would leave compute units idle.  A
+// piece is at least four chunks: its state is formed, joined and read again,
+// which costs about what three chunks' walk does.
+void make_geom(Lin* p, const int32_t* cu) {
+  const int64_t want = 512, T = p->T, C = p->C;
+  const int64_t units = p->packed ? 0 : p->N * p->H;
+  int64_t L;
+  const int64_t whole = (T + C - 1) / C * C;
+  if (p->packed) {
+    L = (T * p->H + want - 1) / want;
+  } else if (units >= want / 2) {
+    L = whole;
+  } else {
+    const int64_t P = (want + units - 1) / units;
+    L = (T + P - 1) / P;
+  }
+  L = (L + C - 1) / C * C;
+  if (L < 4 * C) L = 4 * C;
+  if (L > whole) L = whole > 0 ? whole : C;
+  la::Geom& g = p->g;
+  g.cu = cu;
+  g.N = (int)p->N;
+  g.T = (int)T;
+  g.L = (int)L;
+  g.P = T > 0 ? (int)((T + L - 1) / L) : 1;
+  g.pieces = p->packed ? (int)(T / L + p->N + 1) : (int)(p->N * g.P);
+  g.H = p->H;
+  g.Hk = p->Hk;
+  g.Dk = p->Dk;
+  g.Dv = p->Dv;
+}
+
+int check_lin(int64_t n_seq, int64_t B, int64_t T, int64_t H, int64_t Hk, int64_t Dk, int64_t Dv, int dtype,
+              uint32_t flags, bool packed, const int32_t* cu, Lin* p) {
+  if (dtype != GSPN_F32 && dtype != GSPN_BF16) return GSPN_ERR_DTYPE;
+  if (flags & ~(uint32_t)GSPN_LINATTN_DECAY_PER_TOKEN) return GSPN_ERR_UNSUPPORTED;
+  if (n_seq < 0 || B < 0 || T < 0 || H < 1 || Hk < 1 || Dk < 1 || Dv < 1) return GSPN_ERR_SHAPE;
+  if (H % Hk) return GSPN_ERR_SHAPE;
+  if (packed ? B != 1 : n_seq != B) return GSPN_ERR_SHAPE;
+  if (Dk > la::kMaxDim || Dv > la::kMaxDim || H > 65535) return GSPN_ERR_UNSUPPORTED;
+  if (T > 0x7fff0000LL || B > 0x7fff0000LL || n_seq > 0x7fff0000LL) return GSPN_ERR_UNSUPPORTED;
+  int64_t n;
+  if (!mul_ok(B, T, &n) || !mul_ok(n, H, &n) || !mul_ok(n, 128 * 8, &n) || !mul_ok(n_seq, H, &n) ||
+      !mul_ok(n, 128 * 128 * 4, &n))
+    return GSPN_ERR_SHAPE;
+  *p = Lin{B, T, n_seq, (int)H, (int)Hk, (int)Dk, (int)Dv, dtype, flags, packed, {}, 0, 0, 0};
+  p->KP = la::pad_dim(p->Dk);
+  p->VP = la::pad_dim(p->Dv);
+  p->C = la::chunk_len(dtype);
+  if (n_seq == 0 && !packed) return GSPN_OK;
+  make_geom(p, cu);
+  // pieces and workgroups are counted in 32 bits (the join has 64 a head)
+  const int64_t pieces = packed ? T / p->g.L + n_seq + 1 : n_seq * p->g.P;
+  if (pieces > 0x7fffffffLL / 64 / H) return GSPN_ERR_UNSUPPORTED;
+  return GSPN_OK;
+}
+
+bool cut(const Lin& p) { return p.g.L < p.T; }  // some sequence may have several pieces
+
+struct LinLayout {
+  size_t start, gtot;                       // forward: start states of pieces
+  size_t end, gtot_rev, chunks, dq32, dk32, da;  // backward
+  size_t bytes;
+};
+
+LinLayout lin_layout(const Lin& p, bool bwd) {
+  LinLayout l{};
+  size_t at = 0;
+  const auto take = [&](size_t n) {
+    const size_t r = at;
+    at += round256(n);
+    return r;
+  };
+  const size_t ph = (size_t)p.g.pieces * p.H, st = (size_t)p.KP * p.VP;
+  if (cut(p)) {
+    l.start = take(ph * st * 4);
+    l.gtot = take(ph * 4);
+  }
+  if (bwd) {
+    if (cut(p)) {
+      l.end = take(ph * st * 4);
+      l.gtot_rev = take(ph * 4);
+    }
+    l.chunks = take(ph * (p.g.L / p.C) * st * esize(p.dtype));
+    if (p.H != p.Hk) {
+      l.dq32 = take((size_t)p.B * p.T * p.H * p.Dk * 4);
+      l.dk32 = take((size_t)p.B * p.T * p.H * p.Dk * 4);
+    }
+    if (!(p.flags & GSPN_LINATTN_DECAY_PER_TOKEN)) l.da = take(ph * 4);
+  }
+  l.bytes = at;
+  return l;
+}
+
+bool nothing(const Lin& p) { return p.packed ? p.T == 0 && p.N == 0 : p.N == 0; }
+
+// strides: batch row, token, head of q, k, v (elements); null: contiguous
+int lin_rows(const Lin& p, const void* ptr, int64_t heads, int D, const int64_t* s, la::Rows* r, Span* sp) {
+  const int64_t d[3] = {p.T * heads * D, heads * D, D};
+  if (!s) s = d;
+  if (s[0] < 0 || s[1] < 0 || s[2] < 0) return GSPN_ERR_SHAPE;
+  // the kernels add rows of a piece in 64 bits; the extent has to be a number
+  int64_t e = D, t;
+  const int64_t n[3] = {p.B, p.T, heads};
+  for (int i = 0; i < 3; ++i) {
+    if (n[i] > 0 && (!mul_ok(n[i] - 1, s[i], &t) || t > INT64_MAX / 16 || (e += t) > INT64_MAX / 16))
+      return GSPN_ERR_SHAPE;
+  }
+  const size_t es = esize(p.dtype);
+  const int V = (int)(16 / es);
+  *r = la::Rows{ptr, s[0], s[1], s[2], aligned(ptr, 16) && D % V == 0 && s[0] % V == 0 && s[1] % V == 0 && s[2] % V == 0};
+  *sp = span(ptr, p.B * p.T * heads ? e : 0, es);
+  return GSPN_OK;
+}
+
+hipError_t run_state(const Lin& p, const la::StateArgs& a) {
+  return p.dtype == GSPN_F32 ? la::linattn_state_f32(a) : la::linattn_state_bf16(a);
+}
+
+struct LinInputs {
+  la::Rows q, k, v;
+  Span sq, sk, sv, sa;
+};
+
+int lin_inputs(const Lin& p, const void* q, const void* k, const void* v, const void* a, const int64_t* strides,
+               LinInputs* in) {
+  const bool data = p.B * p.T > 0;
+  if (data && (!q || !k || !v || !a)) return GSPN_ERR_NULL;
+  const size_t es = esize(p.dtype);
+  if (!aligned(q, es) || !aligned(k, es) || !aligned(v, es) || !aligned(a, es)) return GSPN_ERR_ALIGN;
+  int st;
+  if ((st = lin_rows(p, q, p.Hk, p.Dk, strides, &in->q, &in->sq)) ||
+      (st = lin_rows(p, k, p.Hk, p.Dk, strides ? strides + 3 : nullptr, &in->k, &in->sk)) ||
+      (st = lin_rows(p, v, p.H, p.Dv, strides ? strides + 6 : nullptr, &in->v, &in->sv)))
+    return st;
+  in->sa = span(a, (p.flags & GSPN_LINATTN_DECAY_PER_TOKEN) ? p.B * p.T * p.H : p.H, es);
+  return GSPN_OK;
+}
+
+// start states of the pieces (x along the registers)
+hipError_t join_pieces(const Lin& p, la::StateArgs s, const float* s0, float* local, float* gtot, void* stream) {
+  s.mode = 0;
+  s.local = local;
+  s.gtot = gtot;
+  hipError_t e = run_state(p, s);
+  if (e != hipSuccess || p.N == 0) return e;
+  la::JoinArgs j{p.g, local, gtot, s0, s.Dx, s.Dy, s.sx, s.sy, s.reverse, stream};
+  return la::linattn_join(j);
+}
+
+}  // namespace
+
+extern "C" size_t gspn_linattn_fwd_workspace_bytes(int64_t n_seq, int64_t B, int64_t T, int64_t H, int64_t Hk,
+                                                   int64_t Dk, int64_t Dv, int packed, gspn_dtype dtype,
+                                                   uint32_t flags) {
+  Lin p;
+  if (check_lin(n_seq, B, T, H, Hk, Dk, Dv, dtype, flags, packed, nullptr, &p) || nothing(p)) return 0;
+  return lin_layout(p, false).bytes;
+}
+
+extern "C" size_t gspn_linattn_bwd_workspace_bytes(int64_t n_seq, int64_t B, int64_t T, int64_t H, int64_t Hk,
+                                                   int64_t Dk, int64_t Dv, int packed, gspn_dtype dtype,
+                                                   uint32_t flags) {
+  Lin p;
+  if (check_lin(n_seq, B, T, H, Hk, Dk, Dv, dtype, flags, packed, nullptr, &p) || nothing(p)) return 0;
+  return lin_layout(p, true).bytes;
+}
+
+extern "C" int gspn_linattn_fwd(const void* q, const void* k, const void* v, const void* log_decay,
+                                const float* initial_state, const int32_t* cu_seqlens, void* o, float* final_state,
+                                int64_t n_seq, int64_t B, int64_t T, int64_t H, int64_t Hk, int64_t Dk, int64_t Dv,
+                                const int64_t* strides, gspn_dtype dtype, uint32_t flags, float scale,
+                                void* workspace, size_t workspace_bytes, void* stream) {
+  Lin p;
+  int st = check_lin(n_seq, B, T, H, Hk, Dk, Dv, dtype, flags, cu_seqlens != nullptr, cu_seqlens, &p);
+  if (st || nothing(p)) return st;
+  LinInputs in;
+  if ((st = lin_inputs(p, q, k, v, log_decay, strides, &in))) return st;
+  if (B * T > 0 && !o) return GSPN_ERR_NULL;
+  const size_t es = esize(dtype);
+  if (!aligned(o, es) || !aligned(initial_state, 4) || !aligned(final_state, 4) || !aligned(cu_seqlens, 4))
+    return GSPN_ERR_ALIGN;
+  const int64_t states = n_seq * H * Dk * Dv;
+  const Span ins[] = {in.sq, in.sk, in.sv, in.sa, span(initial_state, states, 4),
+                      span(cu_seqlens, n_seq + 1, 4)};
+  const LinLayout l = lin_layout(p, false);
+  if (l.bytes && (!workspace || workspace_bytes < l.bytes)) return GSPN_ERR_WORKSPACE;
+  if (l.bytes && !aligned(workspace, 256)) return GSPN_ERR_ALIGN;
+  const Span outs[] = {span(o, B * T * H * Dv, es), span(final_state, states, 4),
+                       span(l.bytes ? workspace : nullptr, (int64_t)l.bytes, 1)};
+  if ((st = check_spans(ins, outs))) return st;
+  char* ws = (char*)workspace;
+  const int per_token = (flags & GSPN_LINATTN_DECAY_PER_TOKEN) != 0;
+  float* start = cut(p) ? (float*)(ws + l.start) : nullptr;
+  if (cut(p)) {
+    la::StateArgs s{};
+    s.g = p.g; s.x = in.k; s.y = in.v; s.x_shared = 1; s.Dx = p.Dk; s.Dy = p.Dv;
+    s.a = log_decay; s.per_token = per_token; s.scale = scale; s.sx = p.Dv; s.sy = 1; s.stream = stream;
+    if (join_pieces(p, s, initial_state, start, (float*)(ws + l.gtot), stream) != hipSuccess) return GSPN_ERR_HIP;
+  }
+  la::FwdArgs f{};
+  f.g = p.g; f.q = in.q; f.k = in.k; f.v = in.v; f.a = log_decay; f.per_token = per_token; f.scale = scale;
+  f.s0 = initial_state; f.sf = final_state; f.start = start; f.o = o; f.stream = stream;
+  f.ovec = Dv % 4 == 0 && aligned(o, 4 * es);
+  const hipError_t e = dtype == GSPN_F32 ? la::linattn_fwd_f32(f) : la::linattn_fwd_bf16(f);
+  return e == hipSuccess ? GSPN_OK : GSPN_ERR_HIP;
+}
+
+extern "C" int gspn_linattn_bwd(const void* dout, const void* q, const void* k, const void* v, const void* log_decay,
+                                const float* initial_state, const float* dfinal_state, const int32_t* cu_seqlens,
+                                void* dq, void* dk, void* dv, void* dlog_decay, float* dinitial_state, int64_t n_seq,
+                                int64_t B, int64_t T, int64_t H, int64_t Hk, int64_t Dk, int64_t Dv,
+                                const int64_t* strides, gspn_dtype dtype, uint32_t flags, float scale,
+                                void* workspace, size_t workspace_bytes, void* stream) {
+  Lin p;
+  int st = check_lin(n_seq, B, T, H, Hk, Dk, Dv, dtype, flags, cu_seqlens != nullptr, cu_seqlens, &p);
+  if (st || nothing(p)) return st;
+  LinInputs in;
+  if ((st = lin_inputs(p, q, k, v, log_decay, strides, &in))) return st;
+  const int per_token = (flags & GSPN_LINATTN_DECAY_PER_TOKEN) != 0;
+  if (B * T > 0 && (!dout || !dq || !dk || !dv)) return GSPN_ERR_NULL;
+  if ((B * T > 0 || !per_token) && !dlog_decay) return GSPN_ERR_NULL;
+  const size_t es = esize(dtype);
+  for (const void* x : {dout, (const void*)dq, (const void*)dk, (const void*)dv, (const void*)dlog_decay})
+    if (!aligned(x, es)) return GSPN_ERR_ALIGN;
+  for (const void* x : {(const void*)initial_state, (const void*)dfinal_state, (const void*)dinitial_state,
+                        (const void*)cu_seqlens})
+    if (!aligned(x, 4)) return GSPN_ERR_ALIGN;
+  la::Rows rd;
+  Span sd;
+  if ((st = lin_rows(p, dout, H, p.Dv, nullptr, &rd, &sd))) return st;
+  const int64_t states = n_seq * H * Dk * Dv, qk = B * T * Hk * Dk;
+  const LinLayout l = lin_layout(p, true);
+  if (!workspace || workspace_bytes < l.bytes) return GSPN_ERR_WORKSPACE;
+  if (!aligned(workspace, 256)) return GSPN_ERR_ALIGN;
+  const Span ins[] = {in.sq, in.sk, in.sv, in.sa, sd, span(initial_state, states, 4), span(dfinal_state, states, 4),
+                      span(cu_seqlens, n_seq + 1, 4)};
+  const Span outs[] = {span(dq, qk, es), span(dk, qk, es), span(dv, B * T * H * Dv, es),
+                       span(dlog_decay, per_token ? B * T * H : H, es), span(dinitial_state, states, 4),
+                       span(workspace, (int64_t)l.bytes, 1)};
+  if ((st = check_spans(ins, outs))) return st;
+  char* ws = (char*)workspace;
+  // states before each chunk (registers along v, lanes along k)
+  la::StateArgs s{};
+  s.g = p.g; s.x = in.v; s.y = in.k; s.y_shared = 1; s.Dx = p.Dv; s.Dy = p.Dk; s.a = log_decay;
+  s.per_token = per_token; s.scale = scale; s.s0 = initial_state; s.sx = 1; s.sy = p.Dv; s.stream = stream;
+  float *start = cut(p) ? (float*)(ws + l.start) : nullptr, *end = cut(p) ? (float*)(ws + l.end) : nullptr;
+  if (cut(p)) {
+    if (join_pieces(p, s, initial_state, start, (float*)(ws + l.gtot), stream) != hipSuccess) return GSPN_ERR_HIP;
+    la::StateArgs r{};
+    r.g = p.g; r.x = in.q; r.y = rd; r.x_shared = 1; r.Dx = p.Dk; r.Dy = p.Dv; r.a = log_decay;
+    r.per_token = per_token; r.scale = scale; r.reverse = 1; r.sx = p.Dv; r.sy = 1; r.stream = stream;
+    if (join_pieces(p, r, dfinal_state, end, (float*)(ws + l.gtot_rev), stream) != hipSuccess) return GSPN_ERR_HIP;
+  }
+  s.mode = 1;
+  s.local = start;
+  s.chunks = ws + l.chunks;
+  if (run_state(p, s) != hipSuccess) return GSPN_ERR_HIP;
+  const bool shared = p.H != p.Hk;
+  la::BwdArgs b{};
+  b.g = p.g; b.q = in.q; b.k = in.k; b.v = in.v; b.dout = rd; b.a = log_decay; b.per_token = per_token;
+  b.scale = scale; b.dsf = dfinal_state; b.ds0 = dinitial_state; b.end = end; b.chunks = ws + l.chunks;
+  b.dq = dq; b.dk = dk; b.dv = dv; b.da = dlog_decay; b.stream = stream;
+  b.dkvec = Dk % 4 == 0 && (shared || (aligned(dq, 4 * es) && aligned(dk, 4 * es)));
+  b.dvvec = Dv % 4 == 0 && aligned(dv, 4 * es);
+  if (shared) {
+    b.dq32 = (float*)(ws + l.dq32);
+    b.dk32 = (float*)(ws + l.dk32);
+  }
+  if (!per_token) b.da_piece = (float*)(ws + l.da);
+  if ((dtype == GSPN_F32 ? la::linattn_bwd_f32(b) : la::linattn_bwd_bf16(b)) != hipSuccess) return GSPN_ERR_HIP;
+  if (shared || !per_token) {
+    la::ReduceArgs r{};
+    r.tokens = B * T; r.H = p.H; r.Hk = p.Hk; r.Dk = p.Dk; r.dtype = dtype; r.dq32 = b.dq32; r.dk32 = b.dk32;
+    r.dq = dq; r.dk = dk; r.da_piece = b.da_piece; r.da = dlog_decay; r.pieces = p.g.pieces; r.stream = stream;
+    if (la::linattn_reduce(r) != hipSuccess) return GSPN_ERR_HIP;
+  }
+  return GSPN_OK;
+}
+
+extern "C" int gspn_linattn_step(const void* q, const void* k, const void* v, const void* log_decay, float* state,
+                                 const int32_t* slots, void* o, int64_t n_slots, int64_t B, int64_t H, int64_t Hk,
+                                 int64_t Dk, int64_t Dv, const int64_t* strides, gspn_dtype dtype, uint32_t flags,
+                                 float scale, void* stream) {
+  Lin p;
+  int st = check_lin(B, B, 1, H, Hk, Dk, Dv, dtype, flags, false, nullptr, &p);
+  if (st) return st;
+  if (n_slots < 0 || (!slots && n_slots < B)) return GSPN_ERR_SHAPE;
+  int64_t states;
+  if (!mul_ok(n_slots, H * Dk * Dv * 4, &states)) return GSPN_ERR_SHAPE;
+  states = n_slots * H * Dk * Dv;
+  if (B == 0) return GSPN_OK;
+  if (B * H > 0x7fffffffLL) return GSPN_ERR_UNSUPPORTED;
+  int64_t full[9];  // batch row, (token), head
+  if (strides)
+    for (int i = 0; i < 3; ++i) {
+      full[3 * i] = strides[2 * i];
+      full[3 * i + 1] = 0;
+      full[3 * i + 2] = strides[2 * i + 1];
+    }
+  LinInputs in;
+  if ((st = lin_inputs(p, q, k, v, log_decay, strides ? full : nullptr, &in))) return st;
+  if (!o || (n_slots > 0 && !state)) return GSPN_ERR_NULL;
+  const size_t es = esize(dtype);
+  if (!aligned(o, es) || !aligned(state, 16) || !aligned(slots, 4)) return GSPN_ERR_ALIGN;
+  const Span ins[] = {in.sq, in.sk, in.sv, in.sa, span(slots, B, 4)};
+  const Span outs[] = {span(o, B * H * Dv, es), span(state, states, 4)};
+  if ((st = check_spans(ins, outs))) return st;
+  la::StepArgs a{};
+  a.q = in.q; a.k = in.k; a.v = in.v; a.a = log_decay; a.per_row = (flags & GSPN_LINATTN_DECAY_PER_TOKEN) != 0;
+  a.scale = scale; a.state = state; a.slot = slots; a.slots = n_slots; a.o = o; a.B = B; a.H = p.H; a.Hk = p.Hk;
+  a.Dk = p.Dk; a.Dv = p.Dv; a.dtype = dtype; a.stream = stream;
+  return la::linattn_step(a) == hipSuccess ? GSPN_OK : GSPN_ERR_HIP;
+}
+
+// ---------------------------------------------------------------------------
+// group norm
+// ---------------------------------------------------------------------------
+namespace {
+
+int check_norm(int64_t B, int64_t L, int64_t C, int64_t G, int dtype, int act, float eps, int64_t* n) {
+  if (dtype != GSPN_F32 && dtype != GSPN_BF16) return GSPN_ERR_DTYPE;
+  if (B < 0 || L < 0 || C < 1 || G < 1 || C % G) return GSPN_ERR_SHAPE;
+  if (act < GSPN_ACT_NONE || act > GSPN_ACT_GELU) return GSPN_ERR_UNSUPPORTED;
+  if (!(eps >= 0.f) || std::isinf(eps)) return GSPN_ERR_UNSUPPORTED;
+  if (C > gn::kMaxC || L > 0x7fffffffLL) return GSPN_ERR_UNSUPPORTED;
+  if (!mul_ok(B, L, n) || !mul_ok(*n, C, n) || *n > INT64_MAX / 16) return GSPN_ERR_SHAPE;
+  if (B > 0x7fffffffLL / 256 || (B > 0 && G > 0x7fffffffLL / B)) return GSPN_ERR_UNSUPPORTED;
+  return GSPN_OK;
+}
+
+}  // namespace
+
+namespace gspn {
+namespace gn {
+
+size_t fwd_workspace(int64_t B, int64_t L, int C, int G, int dtype) {
+  size_t most = 0;
+  for (int vec = 0; vec < 2; ++vec) {
+    const Plan p = make_plan(B, L, C, G, dtype, vec, false);
+    const size_t n = p.wave ? 0 : round256((size_t)B * p.splits * G * 8);
+    most = n > most ? n : most;
+  }
+  return most;
+}
+size_t bwd_workspace(int64_t B, int64_t L, int C, int G, int dtype) {
+  size_t most = 0;
+  for (int vec = 0; vec < 2; ++vec) {
+    const Plan p = make_plan(B, L, C, G, dtype, vec, true);
+    const size_t n = p.wave ? (size_t)((B + p.rows - 1) / p.rows) * 2 * C * 4
+                            : (size_t)B * p.splits * 2 * C * 4 + (size_t)B * G * 8;
+    most = n > most ? n : most;
+  }
+  return round256(most);
+}
+
+}  // namespace gn
+}  // namespace gspn
+
+extern "C" size_t gspn_group_norm_fwd_workspace_bytes(int64_t B, int64_t L, int64_t C, int64_t G, gspn_dtype dtype) {
+  int64_t n;
+  if (check_norm(B, L, C, G, dtype, 0, 0.f, &n) || n == 0) return 0;
+  return gn::fwd_workspace(B, L, (int)C, (int)G, dtype);
+}
+
+extern "C" size_t gspn_group_norm_bwd_workspace_bytes(int64_t B, int64_t L, int64_t C, int64_t G, gspn_dtype dtype) {
+  int64_t n;
+  if (check_norm(B, L, C, G, dtype, 0, 0.f, &n) || n == 0) return 0;
+  return gn::bwd_workspace(B, L, (int)C, (int)G, dtype);
+}
+
+extern "C" int gspn_group_norm_fwd(const void* x, const void* weight, const void* bias, void* y, float* mean,
+                                   float* rstd, int64_t B, int64_t L, int64_t C, int64_t G, float eps, int act,
+                                   gspn_dtype dtype, void* workspace, size_t workspace_bytes, void* stream) {
+  int64_t n;
+  int st = check_norm(B, L, C, G, dtype, act, eps, &n);
+  if (st || n == 0) return st;
+  if (!x || !y || !mean || !rstd) return GSPN_ERR_NULL;
+  const size_t es = esize(dtype);
+  for (const void* p : {x, weight, bias, (const void*)y})
+    if (!aligned(p, es)) return GSPN_ERR_ALIGN;
+  if (!aligned(mean, 4) || !aligned(rstd, 4)) return GSPN_ERR_ALIGN;
+  const size_t need = gn::fwd_workspace(B, L, (int)C, (int)G, dtype);
+  if (need && (!workspace || workspace_bytes < need)) return GSPN_ERR_WORKSPACE;
+  if (need && !aligned(workspace, 256)) return GSPN_ERR_ALIGN;
+  const Span ins[] = {span(x, n, es), span(weight, C, es), span(bias, C, es)};
+  const Span outs[] = {span(y, n, es), span(mean, B * G, 4), span(rstd, B * G, 4),
+                       span(need ? workspace : nullptr, (int64_t)need, 1)};
+  if ((st = check_spans(ins, outs))) return st;
+  gn::Args a{};
+  a.x = x; a.weight = weight; a.bias = bias; a.eps = eps; a.act = act; a.B = B; a.L = L; a.C = (int)C; a.G = (int)G;
+  a.mean = mean; a.rstd = rstd; a.y = y; a.ws = workspace; a.vec = aligned(x, 16) && aligned(y, 16);
+  a.stream = stream;
+  return (dtype == GSPN_F32 ? gn::fwd_f32(a) : gn::fwd_bf16(a)) == hipSuccess ? GSPN_OK : GSPN_ERR_HIP;
+}
+
+extern "C" int gspn_group_norm_bwd(const void* dy, const void* x, const void* weight, const void* bias,
+                                   const float* mean, const float* rstd, void* dx, void* dweight, void* dbias,
+                                   int64_t B, int64_t L, int64_t C, int64_t G, int act, gspn_dtype dtype,
+                                   void* workspace, size_t workspace_bytes, void* stream) {
+  int64_t n;
+  int st = check_norm(B, L, C, G, dtype, act, 0.f, &n);
+  if (st || n == 0) return st;
+  if (!dy || !x || !mean || !rstd || !dx) return GSPN_ERR_NULL;
+  const size_t es = esize(dtype);
+  for (const void* p : {dy, x, weight, bias, (const void*)dx, (const void*)dweight, (const void*)dbias})
+    if (!aligned(p, es)) return GSPN_ERR_ALIGN;
+  if (!aligned(mean, 4) || !aligned(rstd, 4)) return GSPN_ERR_ALIGN;
+  const size_t need = gn::bwd_workspace(B, L, (int)C, (int)G, dtype);
+  if (!workspace || workspace_bytes < need) return GSPN_ERR_WORKSPACE;
+  if (!aligned(workspace, 256)) return GSPN_ERR_ALIGN;
+  const Span ins[] = {span(dy, n, es), span(x, n, es), span(weight, C, es), span(bias, C, es), span(mean, B * G, 4),
+                      span(rstd, B * G, 4)};
+  const Span outs[] = {span(dx, n, es), span(dweight, C, es), span(dbias, C, es), span(workspace, (int64_t)need, 1)};
+  if ((st = check_spans(ins, outs))) return st;
+  gn::Args a{};
+  a.x = x; a.weight = weight; a.bias = bias; a.act = act; a.B = B; a.L = L; a.C = (int)C; a.G = (int)G;
+  a.mean = const_cast<float*>(mean); a.rstd = const_cast<float*>(rstd); a.dy = dy; a.dx = dx; a.dweight = dweight;
+  a.dbias = dbias; a.ws = workspace; a.vec = aligned(x, 16) && aligned(dy, 16) && aligned(dx, 16); a.stream = stream;
+  return (dtype == GSPN_F32 ? gn::bwd_f32(a) : gn::bwd_bf16(a)) == hipSuccess ? GSPN_OK : GSPN_ERR_HIP;
+}

@@ -19,20 +19,25 @@ GSPN_ALGO_TWO_PASS = 4
 GSPN_FLAG_W_LOGITS, GSPN_FLAG_EDGE_RENORM, GSPN_FLAG_LAM_PER_DIR = 1, 2, 4
 GSPN_FLAG_U_PER_DIR, GSPN_FLAG_Y_PER_DIR, GSPN_FLAG_SAVE_STATE = 8, 16, 32
 GSPN_MAX_LINE = 4096
+GSPN_LINATTN_DECAY_PER_TOKEN = 1
+GSPN_ACT_NONE, GSPN_ACT_SILU, GSPN_ACT_GELU = 0, 1, 2
 STATUS = {0: "GSPN_OK", 1: "GSPN_ERR_NULL", 2: "GSPN_ERR_SHAPE", 3: "GSPN_ERR_MASK",
           4: "GSPN_ERR_DTYPE", 5: "GSPN_ERR_ALIGN", 6: "GSPN_ERR_ALIAS",
           7: "GSPN_ERR_UNSUPPORTED", 8: "GSPN_ERR_WORKSPACE", 9: "GSPN_ERR_HIP"}
 
 # every symbol include/gspn.h declares
 EXPORTS = ("gspn_scan_fwd_workspace_bytes", "gspn_scan_fwd", "gspn_scan_fwd_noalloc",
-           "gspn_scan_bwd_workspace_bytes", "gspn_scan_bwd", "gspn_copy_calibration", "gspn_strerror",
-           "gspn_version")
+           "gspn_scan_bwd_workspace_bytes", "gspn_scan_bwd", "gspn_linattn_fwd_workspace_bytes",
+           "gspn_linattn_fwd", "gspn_linattn_bwd_workspace_bytes", "gspn_linattn_bwd", "gspn_linattn_step",
+           "gspn_group_norm_fwd_workspace_bytes", "gspn_group_norm_fwd", "gspn_group_norm_bwd_workspace_bytes",
+           "gspn_group_norm_bwd", "gspn_copy_calibration", "gspn_strerror", "gspn_version")
 GSPN_NOALLOC_SCRATCH_BYTES = 64 << 20
 
 _lib = None
 
 _p, _i64, _u32, _i, _sz = (ctypes.c_void_p, ctypes.c_int64, ctypes.c_uint32, ctypes.c_int,
                            ctypes.c_size_t)
+_f = ctypes.c_float
 
 
 class GSPNError(RuntimeError):
@@ -63,6 +68,20 @@ def load() -> ctypes.CDLL:
     lib.gspn_scan_bwd.argtypes = [_p, _p, _p, _p, _p, _p, _p, _p, _p, _i64, _i64, _i64, _i64, _u32,
                                   _i, _i64, _i64, _u32, _i, _p, _sz, _p]
     lib.gspn_scan_bwd.restype = _i
+    for fn in (lib.gspn_linattn_fwd_workspace_bytes, lib.gspn_linattn_bwd_workspace_bytes):
+        fn.argtypes = [_i64] * 7 + [_i, _i, _u32]
+        fn.restype = _sz
+    lib.gspn_linattn_fwd.argtypes = [_p] * 8 + [_i64] * 7 + [_p, _i, _u32, _f, _p, _sz, _p]
+    lib.gspn_linattn_bwd.argtypes = [_p] * 13 + [_i64] * 7 + [_p, _i, _u32, _f, _p, _sz, _p]
+    lib.gspn_linattn_step.argtypes = [_p] * 7 + [_i64] * 6 + [_p, _i, _u32, _f, _p]
+    for fn in (lib.gspn_group_norm_fwd_workspace_bytes, lib.gspn_group_norm_bwd_workspace_bytes):
+        fn.argtypes = [_i64] * 4 + [_i]
+        fn.restype = _sz
+    lib.gspn_group_norm_fwd.argtypes = [_p] * 6 + [_i64] * 4 + [_f, _i, _i, _p, _sz, _p]
+    lib.gspn_group_norm_bwd.argtypes = [_p] * 9 + [_i64] * 4 + [_i, _i, _p, _sz, _p]
+    for fn in (lib.gspn_linattn_fwd, lib.gspn_linattn_bwd, lib.gspn_linattn_step, lib.gspn_group_norm_fwd,
+               lib.gspn_group_norm_bwd):
+        fn.restype = _i
     lib.gspn_copy_calibration.argtypes = [_p, _p, _sz, _p]
     lib.gspn_copy_calibration.restype = _i
     lib.gspn_strerror.argtypes = [_i]
@@ -101,6 +120,55 @@ def gspn_scan_bwd(dy, x, w, lam, u, dx, dw, dlam, du, B, C, H, W, mask, dtype, g
                   algo, workspace, workspace_bytes, stream) -> int:
     return int(load().gspn_scan_bwd(dy, x, w, lam, u, dx, dw, dlam, du, B, C, H, W, mask, dtype,
                                     group_h, group_w, flags, algo, workspace, workspace_bytes, stream))
+
+
+def gspn_linattn_fwd_workspace_bytes(n_seq, B, T, H, Hk, Dk, Dv, packed, dtype, flags=0) -> int:
+    return int(load().gspn_linattn_fwd_workspace_bytes(n_seq, B, T, H, Hk, Dk, Dv, packed, dtype, flags))
+
+
+def gspn_linattn_bwd_workspace_bytes(n_seq, B, T, H, Hk, Dk, Dv, packed, dtype, flags=0) -> int:
+    return int(load().gspn_linattn_bwd_workspace_bytes(n_seq, B, T, H, Hk, Dk, Dv, packed, dtype, flags))
+
+
+def gspn_linattn_fwd(q, k, v, log_decay, initial_state, cu_seqlens, o, final_state, n_seq, B, T, H, Hk, Dk, Dv,
+                     strides, dtype, flags, scale, workspace, workspace_bytes, stream) -> int:
+    return int(load().gspn_linattn_fwd(q, k, v, log_decay, initial_state, cu_seqlens, o, final_state, n_seq, B, T,
+                                       H, Hk, Dk, Dv, strides, dtype, flags, scale, workspace, workspace_bytes,
+                                       stream))
+
+
+def gspn_linattn_bwd(dout, q, k, v, log_decay, initial_state, dfinal_state, cu_seqlens, dq, dk, dv, dlog_decay,
+                     dinitial_state, n_seq, B, T, H, Hk, Dk, Dv, strides, dtype, flags, scale, workspace,
+                     workspace_bytes, stream) -> int:
+    return int(load().gspn_linattn_bwd(dout, q, k, v, log_decay, initial_state, dfinal_state, cu_seqlens, dq, dk,
+                                       dv, dlog_decay, dinitial_state, n_seq, B, T, H, Hk, Dk, Dv, strides, dtype,
+                                       flags, scale, workspace, workspace_bytes, stream))
+
+
+def gspn_linattn_step(q, k, v, log_decay, state, slots, o, n_slots, B, H, Hk, Dk, Dv, strides, dtype, flags, scale,
+                      stream) -> int:
+    return int(load().gspn_linattn_step(q, k, v, log_decay, state, slots, o, n_slots, B, H, Hk, Dk, Dv, strides,
+                                        dtype, flags, scale, stream))
+
+
+def gspn_group_norm_fwd_workspace_bytes(B, L, C, G, dtype) -> int:
+    return int(load().gspn_group_norm_fwd_workspace_bytes(B, L, C, G, dtype))
+
+
+def gspn_group_norm_bwd_workspace_bytes(B, L, C, G, dtype) -> int:
+    return int(load().gspn_group_norm_bwd_workspace_bytes(B, L, C, G, dtype))
+
+
+def gspn_group_norm_fwd(x, weight, bias, y, mean, rstd, B, L, C, G, eps, act, dtype, workspace, workspace_bytes,
+                        stream) -> int:
+    return int(load().gspn_group_norm_fwd(x, weight, bias, y, mean, rstd, B, L, C, G, eps, act, dtype, workspace,
+                                          workspace_bytes, stream))
+
+
+def gspn_group_norm_bwd(dy, x, weight, bias, mean, rstd, dx, dweight, dbias, B, L, C, G, act, dtype, workspace,
+                        workspace_bytes, stream) -> int:
+    return int(load().gspn_group_norm_bwd(dy, x, weight, bias, mean, rstd, dx, dweight, dbias, B, L, C, G, act,
+                                          dtype, workspace, workspace_bytes, stream))
 
 
 def gspn_copy_calibration(src, dst, nbytes, stream) -> int:

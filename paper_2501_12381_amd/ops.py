@@ -24,6 +24,8 @@ from functools import lru_cache
 import torch
 
 from . import lib as L
+from .seq import (GSPNGroupNorm, GSPNLinAttn, gspn_group_norm, gspn_group_norm_bwd,  # noqa: F401
+                  gspn_group_norm_fwd, gspn_linattn, gspn_linattn_bwd, gspn_linattn_fwd, gspn_linattn_step)
 
 _DT = {torch.float32: L.GSPN_F32, torch.bfloat16: L.GSPN_BF16}
 
