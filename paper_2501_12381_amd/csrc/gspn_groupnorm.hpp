@@ -37,41 +37,72 @@ hipError_t bwd_bf16(const Args& a);
 constexpr int kMaxC = 8192;
 
 // ---- how a problem is cut (host; the workspace sizes go by it) ----------------
-// Slabs (one group of one batch entry) that a wave holds in its registers take
-// one launch; larger ones are summed in splits of the L axis and normalised by a
-// second launch.
+// A slab (one group of one batch entry) that fits the registers of a team of
+// threads takes one launch; a larger one is summed in splits of the L axis and
+// normalised by a second launch.
+//
+// Loads are V values wide, the widest that divides a group's channels.  A team
+// covers RT whole rows of its group (cpv loads each) and comes around K times, so a
+// thread has the same channels in all its rows.
 struct Plan {
-  bool wave;       // a wave holds a slab
-  int V, K;        // elements of a load, loads a lane
-  int rows;        // wave: batch entries a wave takes (backward: for one partial sum)
-  int splits;      // else: parts of L
+  bool team;
+  int V, cpv;
+  int NT;          // threads of a team (64: LP lanes of a wave)
+  int LP, K;
+  int rows;        // batch entries a team takes one after another (a partial sum each team in the backward)
+  int splits;      // not team: parts of L
 };
+
+// loads that a thread of a team holds in registers (fp32; the backward holds two
+// tensors; 16 waves of a team share a SIMD's registers by four)
+constexpr int team_loads(int V, int NT, bool bwd) {
+  const int n = 64 / (bwd ? 2 : 1) / (NT == 1024 ? 2 : 1) / V;
+  const int most = NT == 1024 ? 8 : 16;
+  return n < most ? n : most;
+}
 
 inline Plan make_plan(int64_t B, int64_t L, int C, int G, int dtype, int vec, bool bwd) {
   Plan p{};
-  const int cpg = C / G, full = dtype == 0 ? 4 : 8;
-  const int64_t m = L * cpg;
-  const int V = vec && cpg % full == 0 ? full : 1;
-  const int64_t per = (m / V + 63) / 64;  // loads a lane
-  const int most = V == 1 ? 16 : (bwd ? 4 : 8);
-  if (per <= most) {
-    p.wave = true;
-    p.V = V;
+  const int cpg = C / G, full = vec ? (dtype == 0 ? 4 : 8) : 1;
+  p.V = full;
+  while (cpg % p.V) p.V /= 2;
+  p.cpv = cpg / p.V;
+  const int64_t slabs = B * G;
+  if (L * p.cpv <= 32) {
+    p.team = true;
+    p.NT = 64;
     p.K = 1;
-    while (p.K < per) p.K *= 2;
+    p.LP = 1;
+    while (p.LP < L * p.cpv) p.LP *= 2;
+  } else {
+    // the smallest team whose registers hold the slab; a larger one where that
+    // leaves the card with few waves, each with many loads
+    for (int NT = 64; NT <= 1024 && !p.team; NT *= 4) {
+      if (p.cpv > NT) continue;
+      const int RT = NT / p.cpv;
+      const int64_t K = (L + RT - 1) / RT;
+      if (K > team_loads(p.V, NT, bwd) || (NT < 1024 && K > 2 && slabs * (NT / 64) < 2048)) continue;
+      p.team = true;
+      p.NT = NT;
+      p.LP = 64;
+      p.K = 1;
+      while (p.K < K) p.K *= 2;
+    }
+  }
+  if (p.team) {
+    // the parameters are read, and in the backward a partial sum is written, once
+    // for all of a team's entries: as many as leave two waves a SIMD
     p.rows = 1;
-    // backward: the sums over the batch are kept in registers over several
-    // entries, which leaves fewer partial sums; enough waves stay to fill the card
-    if (bwd)
-      while (p.rows < 64 && B * G / (p.rows * 2) >= 4096) p.rows *= 2;
+    const int64_t waves = p.NT == 64 ? (slabs * p.LP + 63) / 64 : slabs * (p.NT / 64);
+    while (p.rows < 64 && waves / (2 * p.rows) >= 2048) p.rows *= 2;
     return p;
   }
-  p.V = vec && C % full == 0 ? full : 1;
-  // four workgroups a compute unit, at least 16 rows each
-  int64_t s = (1024 + B - 1) / B;
+  p.V = full;
+  while (C % p.V) p.V /= 2;
+  // one workgroup of 1024 a compute unit, at least 16 rows each
+  int64_t s = (256 + B - 1) / B;
   const int64_t most_s = (L + 15) / 16;
   if (s > most_s) s = most_s;
-  if (s > 256) s = 256;
   p.splits = (int)(s < 1 ? 1 : s);
   return p;
 }

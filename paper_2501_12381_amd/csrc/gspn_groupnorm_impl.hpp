@@ -15,31 +15,20 @@
 namespace gspn {
 namespace gn {
 
+// V values, aligned to their whole size
+template <typename T, int V> struct __align__(V * sizeof(T)) Pack {
+  T e[V];
+};
 template <typename T, int V> __device__ __forceinline__ void load_v(const T* p, float* x) {
-  if constexpr (V == 1) {
-    x[0] = to_f(p[0]);
-  } else {
-    union {
-      uint4 r;
-      T e[V];
-    } u;
-    u.r = *reinterpret_cast<const uint4*>(p);
+  const Pack<T, V> u = *reinterpret_cast<const Pack<T, V>*>(p);
 #pragma unroll
-    for (int j = 0; j < V; ++j) x[j] = to_f(u.e[j]);
-  }
+  for (int j = 0; j < V; ++j) x[j] = to_f(u.e[j]);
 }
 template <typename T, int V> __device__ __forceinline__ void store_v(T* p, const float* x) {
-  if constexpr (V == 1) {
-    p[0] = from_f<T>(x[0]);
-  } else {
-    union {
-      uint4 r;
-      T e[V];
-    } u;
+  Pack<T, V> u;
 #pragma unroll
-    for (int j = 0; j < V; ++j) u.e[j] = from_f<T>(x[j]);
-    *reinterpret_cast<uint4*>(p) = u.r;
-  }
+  for (int j = 0; j < V; ++j) u.e[j] = from_f<T>(x[j]);
+  *reinterpret_cast<Pack<T, V>*>(p) = u;
 }
 
 __device__ __forceinline__ float sigmoid_f(float z) { return __builtin_amdgcn_rcpf(1.f + __expf(-z)); }
@@ -78,176 +67,221 @@ template <typename T> __device__ __forceinline__ float param(const void* p, int 
 }
 
 // ---------------------------------------------------------------------------
-// slabs that a wave holds: K loads of V values a lane, one launch
+// slabs that a team holds in registers, one launch
 // ---------------------------------------------------------------------------
-// Value e of a slab is channel e % cpg of row e / cpg; neighbouring waves take
-// neighbouring groups, so that together they read whole rows.
-template <typename T, int V, int K> __global__ void __launch_bounds__(256) gn_wave_fwd_kernel(Args A) {
-  const int lane = threadIdx.x & 63;
-  const int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (i >= A.B * A.G) return;
-  const int64_t b = i / A.G;
-  const int gi = (int)(i - b * A.G), cpg = A.C / A.G, m = (int)A.L * cpg;
-  const T* x = reinterpret_cast<const T*>(A.x) + b * A.L * A.C + gi * cpg;
-  T* y = reinterpret_cast<T*>(A.y) + b * A.L * A.C + gi * cpg;
-  float v[K][V];
-  const float p = to_f(x[0]);
-  float s = 0.f, q = 0.f;
-#pragma unroll
-  for (int k = 0; k < K; ++k) {
-    const int e = (k * 64 + lane) * V;
-    if (e < m) load_v<T, V>(x + (int64_t)(e / cpg) * A.C + e % cpg, v[k]);
-    else
-#pragma unroll
-      for (int j = 0; j < V; ++j) v[k][j] = p;
-  }
-#pragma unroll
-  for (int k = 0; k < K; ++k)
-#pragma unroll
-    for (int j = 0; j < V; ++j) s += v[k][j] - p;
-  s = wave_sum(s);
-  const float inv_m = 1.f / (float)m, mean = p + s * inv_m;
-  // the values are here: the squares go around the mean itself
-#pragma unroll
-  for (int k = 0; k < K; ++k)
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const float d = v[k][j] - mean;
-      q += (k * 64 + lane) * V < m ? d * d : 0.f;
+// Thread t of a team: load t % cpv of rows t / cpv + k RT of its group.
+template <int V, int K, int NT> struct Team {
+  int t, RT, r0, c, g;
+  int64_t b0, b1, team;
+  bool on;
+  __device__ __forceinline__ Team(const Args& A, int LP, int cpv, int rows) {
+    int n;
+    if constexpr (NT == 64) {
+      const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+      n = LP;
+      t = (int)(i & (LP - 1));
+      team = i / LP;
+    } else {
+      n = NT;
+      t = threadIdx.x;
+      team = blockIdx.x;
     }
-  q = wave_sum(q);
-  const float rstd = rsqrtf(q * inv_m + A.eps);
-  if (lane == 0) {
-    A.mean[i] = mean;
-    A.rstd[i] = rstd;
+    RT = n / cpv;
+    r0 = t / cpv;
+    c = (t - r0 * cpv) * V;
+    const int64_t part = team / A.G;
+    g = (int)(team - part * A.G);
+    b0 = part * rows;
+    b1 = min(A.B, b0 + rows);
+    on = r0 < RT && b0 < A.B;
   }
+  __device__ __forceinline__ bool has(int k, int64_t L) const { return on && r0 + k * RT < L; }
+};
+
+// sum over a team, in every thread of it; `red`: NT / 64 floats
+template <int NT> __device__ __forceinline__ float team_sum(float v, int LP, float* red) {
+  if constexpr (NT == 64) {
+    for (int k = 1; k < LP; k <<= 1) v += __shfl_xor(v, k);
+    return v;
+  } else {
+    v = wave_sum(v);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+    __syncthreads();
+    float s = 0.f;
 #pragma unroll
-  for (int k = 0; k < K; ++k) {
-    const int e = (k * 64 + lane) * V;
-    if (e < m) {
-      const int c = e % cpg;
-      float w[V], o[V];
+    for (int i = 0; i < NT / 64; ++i) s += red[i];
+    return s;
+  }
+}
+
+// R: batch entries whose loads are in flight together (teams of a few lanes have little else to wait with)
+template <typename T, int V, int K, int NT, int R>
+__global__ void __launch_bounds__(NT < 256 ? 256 : NT) gn_team_fwd_kernel(Args A, int LP, int cpv, int rows) {
+  __shared__ float red[NT / 64];
+  const Team<V, K, NT> m(A, LP, cpv, rows);
+  const int cpg = A.C / A.G, ch = m.g * cpg + m.c;
+  const float inv_m = 1.f / ((float)A.L * (float)cpg);
+  float w[V], bias[V];
 #pragma unroll
-      for (int j = 0; j < V; ++j) w[j] = param<T>(A.weight, gi * cpg + c + j, 1.f);
+  for (int j = 0; j < V; ++j) {
+    w[j] = m.on ? param<T>(A.weight, ch + j, 1.f) : 0.f;
+    bias[j] = m.on ? param<T>(A.bias, ch + j, 0.f) : 0.f;
+  }
+  for (int64_t b = m.b0; b < m.b1; b += R) {
+    float v[R][K][V], p[R];
 #pragma unroll
-      for (int j = 0; j < V; ++j)
-        o[j] = act_f(__builtin_fmaf((v[k][j] - mean) * rstd, w[j], param<T>(A.bias, gi * cpg + c + j, 0.f)), A.act);
-      store_v<T, V>(y + (int64_t)(e / cpg) * A.C + c, o);
+    for (int i = 0; i < R; ++i) {
+      const int64_t bi = min(b + i, m.b1 - 1);  // entries past the last are computed again and not stored
+      const T* x = reinterpret_cast<const T*>(A.x) + bi * A.L * A.C;
+      p[i] = to_f(x[m.g * cpg]);
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        if (m.has(k, A.L)) load_v<T, V>(x + (int64_t)(m.r0 + k * m.RT) * A.C + ch, v[i][k]);
+        else
+#pragma unroll
+          for (int j = 0; j < V; ++j) v[i][k][j] = p[i];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      float s = 0.f, q = 0.f;
+#pragma unroll
+      for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int j = 0; j < V; ++j) s += v[i][k][j] - p[i];
+      const float mean = p[i] + team_sum<NT>(s, LP, red) * inv_m;
+      // the values are here: the squares go around the mean itself
+#pragma unroll
+      for (int k = 0; k < K; ++k)
+        if (m.has(k, A.L))
+#pragma unroll
+          for (int j = 0; j < V; ++j) {
+            const float d = v[i][k][j] - mean;
+            q = __builtin_fmaf(d, d, q);
+          }
+      const float rstd = rsqrtf(team_sum<NT>(q, LP, red) * inv_m + A.eps);
+      if (b + i < m.b1) {
+        if (m.t == 0) {
+          A.mean[(b + i) * A.G + m.g] = mean;
+          A.rstd[(b + i) * A.G + m.g] = rstd;
+        }
+        T* y = reinterpret_cast<T*>(A.y) + (b + i) * A.L * A.C + ch;
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+          if (m.has(k, A.L)) {
+            float o[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j) o[j] = act_f(__builtin_fmaf((v[i][k][j] - mean) * rstd, w[j], bias[j]), A.act);
+            store_v<T, V>(y + (int64_t)(m.r0 + k * m.RT) * A.C, o);
+          }
+      }
     }
   }
 }
 
-// backward; `rows` batch entries a wave, sums over them to ws[part][2][C]
-template <typename T, int V, int K> __global__ void __launch_bounds__(256) gn_wave_bwd_kernel(Args A, int rows) {
-  extern __shared__ float lds[];  // a wave's dw and db of every value of the slab
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t i = (int64_t)blockIdx.x * 4 + wave, parts = (A.B + rows - 1) / rows;
-  const int cpg = A.C / A.G, m = (int)A.L * cpg;
-  const int64_t part = i / A.G;
-  const int gi = (int)(i - part * A.G);
-  const bool on = part < parts;
-  float aw[K][V], ab[K][V], w[K][V], bias[K][V];
+// backward; the sums over a team's entries go to ws[part][2][C]
+template <typename T, int V, int K, int NT, int R>
+__global__ void __launch_bounds__(NT < 256 ? 256 : NT) gn_team_bwd_kernel(Args A, int LP, int cpv, int rows) {
+  __shared__ float red[NT / 64], lds[2][(NT < 256 ? 256 : NT) * V];
+  const Team<V, K, NT> m(A, LP, cpv, rows);
+  const int cpg = A.C / A.G, ch = m.g * cpg + m.c;
+  const float inv_m = 1.f / ((float)A.L * (float)cpg);
+  float w[V], bias[V], aw[V], ab[V];
 #pragma unroll
-  for (int k = 0; k < K; ++k) {
-    const int e = (k * 64 + lane) * V, c = gi * cpg + e % cpg;
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-      aw[k][j] = ab[k][j] = 0.f;
-      w[k][j] = on && e < m ? param<T>(A.weight, c + j, 1.f) : 0.f;
-      bias[k][j] = on && e < m && A.act ? param<T>(A.bias, c + j, 0.f) : 0.f;
-    }
+  for (int j = 0; j < V; ++j) {
+    w[j] = m.on ? param<T>(A.weight, ch + j, 1.f) : 0.f;
+    bias[j] = m.on && A.act ? param<T>(A.bias, ch + j, 0.f) : 0.f;
+    aw[j] = ab[j] = 0.f;
   }
-  const float inv_m = 1.f / (float)m;
-  if (on)
-    for (int64_t b = part * rows; b < min(A.B, (part + 1) * rows); ++b) {
-      const int64_t base = b * A.L * A.C + gi * cpg;
-      const T *x = reinterpret_cast<const T*>(A.x) + base, *dy = reinterpret_cast<const T*>(A.dy) + base;
-      T* dx = reinterpret_cast<T*>(A.dx) + base;
-      const float mean = A.mean[b * A.G + gi], rstd = A.rstd[b * A.G + gi];
-      float xh[K][V], dz[K][V], s1 = 0.f, s2 = 0.f;
+  for (int64_t b = m.b0; b < m.b1; b += R) {
+    float xh[R][K][V], dz[R][K][V], mean[R], rstd[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const int64_t bi = min(b + i, m.b1 - 1);
+      const bool live = b + i < m.b1;
+      mean[i] = A.mean[bi * A.G + m.g];
+      rstd[i] = A.rstd[bi * A.G + m.g];
+      const T *x = reinterpret_cast<const T*>(A.x) + bi * A.L * A.C + ch,
+              *dy = reinterpret_cast<const T*>(A.dy) + bi * A.L * A.C + ch;
 #pragma unroll
       for (int k = 0; k < K; ++k) {
-        const int e = (k * 64 + lane) * V;
-        if (e < m) {
-          const int64_t at = (int64_t)(e / cpg) * A.C + e % cpg;
-          load_v<T, V>(x + at, xh[k]);
-          load_v<T, V>(dy + at, dz[k]);
+        if (m.has(k, A.L) && live) {
+          load_v<T, V>(x + (int64_t)(m.r0 + k * m.RT) * A.C, xh[i][k]);
+          load_v<T, V>(dy + (int64_t)(m.r0 + k * m.RT) * A.C, dz[i][k]);
         } else {
 #pragma unroll
           for (int j = 0; j < V; ++j) {
-            xh[k][j] = mean;
-            dz[k][j] = 0.f;
+            xh[i][k][j] = mean[i];
+            dz[i][k][j] = 0.f;
           }
         }
       }
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      float s1 = 0.f, s2 = 0.f;
 #pragma unroll
       for (int k = 0; k < K; ++k)
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-          xh[k][j] = (xh[k][j] - mean) * rstd;
-          if (A.act) dz[k][j] *= act_slope(__builtin_fmaf(xh[k][j], w[k][j], bias[k][j]), A.act);
-          ab[k][j] += dz[k][j];
-          aw[k][j] = __builtin_fmaf(dz[k][j], xh[k][j], aw[k][j]);
-          const float d = dz[k][j] * w[k][j];
-          s1 += d;
-          s2 = __builtin_fmaf(d, xh[k][j], s2);
+          xh[i][k][j] = (xh[i][k][j] - mean[i]) * rstd[i];
+          if (A.act) dz[i][k][j] *= act_slope(__builtin_fmaf(xh[i][k][j], w[j], bias[j]), A.act);
+          ab[j] += dz[i][k][j];
+          aw[j] = __builtin_fmaf(dz[i][k][j], xh[i][k][j], aw[j]);
+          dz[i][k][j] *= w[j];
+          s1 += dz[i][k][j];
+          s2 = __builtin_fmaf(dz[i][k][j], xh[i][k][j], s2);
         }
-      s1 = wave_sum(s1) * inv_m;
-      s2 = wave_sum(s2) * inv_m;
+      s1 = team_sum<NT>(s1, LP, red) * inv_m;
+      s2 = team_sum<NT>(s2, LP, red) * inv_m;
+      if (b + i < m.b1) {
+        T* dx = reinterpret_cast<T*>(A.dx) + (b + i) * A.L * A.C + ch;
 #pragma unroll
-      for (int k = 0; k < K; ++k) {
-        const int e = (k * 64 + lane) * V;
-        if (e < m) {
-          float o[V];
+        for (int k = 0; k < K; ++k)
+          if (m.has(k, A.L)) {
+            float o[V];
 #pragma unroll
-          for (int j = 0; j < V; ++j) o[j] = rstd * (dz[k][j] * w[k][j] - s1 - xh[k][j] * s2);
-          store_v<T, V>(dx + (int64_t)(e / cpg) * A.C + e % cpg, o);
-        }
+            for (int j = 0; j < V; ++j) o[j] = rstd[i] * (dz[i][k][j] - s1 - xh[i][k][j] * s2);
+            store_v<T, V>(dx + (int64_t)(m.r0 + k * m.RT) * A.C, o);
+          }
       }
     }
-  // sums over the L rows of the slab, channel by channel
-  float* out = reinterpret_cast<float*>(A.ws) + part * 2 * A.C + gi * cpg;
-  if (A.L == 1) {
+  }
+  // sums over the team's RT rows, channel by channel
+  float* out = reinterpret_cast<float*>(A.ws) + m.b0 / rows * 2 * A.C + m.g * cpg;
+  if (m.RT == 1) {
+    if (m.on)
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const int e = (k * 64 + lane) * V;
-#pragma unroll
-      for (int j = 0; j < V; ++j)
-        if (on && e < m) {
-          out[e + j] = aw[k][j];
-          out[A.C + e + j] = ab[k][j];
-        }
-    }
+      for (int j = 0; j < V; ++j) {
+        out[m.c + j] = aw[j];
+        out[A.C + m.c + j] = ab[j];
+      }
     return;
   }
-  float* sw = lds + wave * 2 * m;
 #pragma unroll
-  for (int k = 0; k < K; ++k) {
-    const int e = (k * 64 + lane) * V;
-#pragma unroll
-    for (int j = 0; j < V; ++j)
-      if (e < m) {
-        sw[e + j] = aw[k][j];
-        sw[m + e + j] = ab[k][j];
-      }
+  for (int j = 0; j < V; ++j) {
+    lds[0][threadIdx.x * V + j] = aw[j];
+    lds[1][threadIdx.x * V + j] = ab[j];
   }
   __syncthreads();
-  if (on)
-    for (int c = lane; c < 2 * cpg; c += 64) {
-      const float* p = sw + (c < cpg ? c : m + c - cpg);
-      float t = 0.f;
-      for (int r = 0; r < (int)A.L; ++r) t += p[r * cpg];
-      out[c < cpg ? c : A.C + c - cpg] = t;
-    }
+  if (m.b0 >= A.B) return;
+  const int base = (threadIdx.x - m.t) * V, n = NT == 64 ? LP : NT;
+  for (int c = m.t; c < 2 * cpg; c += n) {
+    const float* p = lds[c < cpg ? 0 : 1] + base + (c < cpg ? c : c - cpg);
+    float s = 0.f;
+    for (int r = 0; r < m.RT; ++r) s += p[r * cpg];
+    out[c < cpg ? c : A.C + c - cpg] = s;
+  }
 }
 
 // dw, db: sums of `parts` partial sums ws[part][2][C]
-template <typename T> __global__ void __launch_bounds__(256) gn_param_kernel(Args A, int64_t parts) {
-  __shared__ float red[2][256];
+template <typename T> __global__ void __launch_bounds__(1024) gn_param_kernel(Args A, int64_t parts) {
+  __shared__ float red[2][1024];
   const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5, c = blockIdx.x * 32 + tx;
   float w = 0.f, b = 0.f;
   if (c < A.C)
-    for (int64_t p = ty; p < parts; p += 8) {
+    for (int64_t p = ty; p < parts; p += 32) {
       const float* s = reinterpret_cast<const float*>(A.ws) + p * 2 * A.C + c;
       w += s[0];
       b += s[A.C];
@@ -257,7 +291,7 @@ template <typename T> __global__ void __launch_bounds__(256) gn_param_kernel(Arg
   __syncthreads();
   if (ty == 0 && c < A.C) {
 #pragma unroll
-    for (int i = 1; i < 8; ++i) {
+    for (int i = 1; i < 32; ++i) {
       w += red[0][i * 32 + tx];
       b += red[1][i * 32 + tx];
     }
@@ -269,8 +303,9 @@ template <typename T> __global__ void __launch_bounds__(256) gn_param_kernel(Arg
 // ---------------------------------------------------------------------------
 // larger slabs: parts of the L axis
 // ---------------------------------------------------------------------------
-// A workgroup of 256 takes rows [r0, r1) of a batch entry, all channels: TX
-// threads side by side on the channels (V each), 256 / TX rows at a time.
+// A workgroup takes rows [r0, r1) of a batch entry, all channels: TX threads side
+// by side on the channels (V each), kThreads / TX rows at a time.
+constexpr int kThreads = 1024;
 struct Tile {
   int nvec, TX, TY, tx, ty;
   bool on;
@@ -279,8 +314,8 @@ struct Tile {
 template <int V> __device__ __forceinline__ Tile make_tile(const Args& A, int split, int splits) {
   Tile t;
   t.nvec = A.C / V;
-  t.TX = min(t.nvec, 256);
-  t.TY = 256 / t.TX;
+  t.TX = min(t.nvec, kThreads);
+  t.TY = kThreads / t.TX;
   t.ty = threadIdx.x / t.TX;
   t.tx = threadIdx.x - t.ty * t.TX;
   t.on = t.ty < t.TY;
@@ -290,7 +325,7 @@ template <int V> __device__ __forceinline__ Tile make_tile(const Args& A, int sp
 }
 
 // parts of the sums: part[b][split][g] = sums of x - p, (x - p)^2
-template <typename T, int V> __global__ void __launch_bounds__(256) gn_stats_kernel(Args A, int splits) {
+template <typename T, int V> __global__ void __launch_bounds__(kThreads) gn_stats_kernel(Args A, int splits) {
   extern __shared__ float red[];  // [TY][C][2]
   const int split = blockIdx.x % splits;
   const int64_t b = blockIdx.x / splits;
@@ -325,7 +360,7 @@ template <typename T, int V> __global__ void __launch_bounds__(256) gn_stats_ker
   __syncthreads();
   const int lane = threadIdx.x & 63;
   float* part = reinterpret_cast<float*>(A.ws) + (int64_t)blockIdx.x * A.G * 2;
-  for (int g = threadIdx.x >> 6; g < A.G; g += 4) {
+  for (int g = threadIdx.x >> 6; g < A.G; g += kThreads / 64) {
     float s = 0.f, q = 0.f;
     for (int i = lane; i < cpg * t.TY; i += 64) {
       const int at = (i / cpg * A.C + g * cpg + i % cpg) * 2;
@@ -341,7 +376,7 @@ template <typename T, int V> __global__ void __launch_bounds__(256) gn_stats_ker
   }
 }
 
-template <typename T, int V> __global__ void __launch_bounds__(256) gn_apply_kernel(Args A, int splits) {
+template <typename T, int V> __global__ void __launch_bounds__(kThreads) gn_apply_kernel(Args A, int splits) {
   extern __shared__ float st[];  // [G] mean, [G] rstd
   const int split = blockIdx.x % splits;
   const int64_t b = blockIdx.x / splits;
@@ -351,7 +386,7 @@ template <typename T, int V> __global__ void __launch_bounds__(256) gn_apply_ker
   T* y = reinterpret_cast<T*>(A.y) + b * A.L * A.C;
   const float inv_m = 1.f / ((float)A.L * (float)cpg);
   const float* part = reinterpret_cast<const float*>(A.ws) + b * splits * A.G * 2;
-  for (int g = threadIdx.x >> 6; g < A.G; g += 4) {
+  for (int g = threadIdx.x >> 6; g < A.G; g += kThreads / 64) {
     float s = 0.f, q = 0.f;
     for (int i = lane; i < splits; i += 64) {
       s += part[((int64_t)i * A.G + g) * 2];
@@ -393,7 +428,7 @@ template <typename T, int V> __global__ void __launch_bounds__(256) gn_apply_ker
 }
 
 // backward, first launch: part[b][split][2][C] = sums over the rows of dz xh, dz
-template <typename T, int V> __global__ void __launch_bounds__(256) gn_bwd_sums_kernel(Args A, int splits) {
+template <typename T, int V> __global__ void __launch_bounds__(kThreads) gn_bwd_sums_kernel(Args A, int splits) {
   extern __shared__ float red[];  // [TY][C][2]
   const int split = blockIdx.x % splits;
   const int64_t b = blockIdx.x / splits;
@@ -433,7 +468,7 @@ template <typename T, int V> __global__ void __launch_bounds__(256) gn_bwd_sums_
     }
   __syncthreads();
   float* part = reinterpret_cast<float*>(A.ws) + (int64_t)blockIdx.x * 2 * A.C;
-  for (int c = threadIdx.x; c < A.C; c += 256) {
+  for (int c = threadIdx.x; c < A.C; c += kThreads) {
     float w = 0.f, d = 0.f;
     for (int y = 0; y < t.TY; ++y) {
       w += red[((int64_t)y * A.C + c) * 2];
@@ -447,32 +482,46 @@ template <typename T, int V> __global__ void __launch_bounds__(256) gn_bwd_sums_
 // second launch, one workgroup a (batch entry, group): S1, S2 to sums[b][g][2] and
 // the channel sums of the entry to its first split's place
 template <typename T> __global__ void __launch_bounds__(256) gn_bwd_group_kernel(Args A, int splits, float* sums) {
-  __shared__ float red[2][4];
-  const int g = blockIdx.x % A.G;
+  __shared__ float red[2][256];
+  const int g = blockIdx.x % A.G, tid = threadIdx.x;
   const int64_t b = blockIdx.x / A.G;
-  const int cpg = A.C / A.G;
+  const int cpg = A.C / A.G, CW = min(cpg, 256), TS = 256 / CW, ts = tid / CW, tc = tid - ts * CW;
   float* part = reinterpret_cast<float*>(A.ws) + b * splits * 2 * A.C + g * cpg;
   float s1 = 0.f, s2 = 0.f;
-  for (int c = threadIdx.x; c < cpg; c += 256) {
+  for (int c0 = 0; c0 < cpg; c0 += CW) {
+    const int c = c0 + tc;
     float w = 0.f, d = 0.f;
-    for (int i = 0; i < splits; ++i) {
-      w += part[(int64_t)i * 2 * A.C + c];
-      d += part[(int64_t)i * 2 * A.C + A.C + c];
+    if (ts < TS && c < cpg)
+#pragma unroll 4
+      for (int i = ts; i < splits; i += TS) {
+        w += part[(int64_t)i * 2 * A.C + c];
+        d += part[(int64_t)i * 2 * A.C + A.C + c];
+      }
+    __syncthreads();
+    red[0][tid] = w;
+    red[1][tid] = d;
+    __syncthreads();
+    if (ts == 0 && c < cpg) {
+      for (int i = 1; i < TS; ++i) {
+        w += red[0][i * CW + tc];
+        d += red[1][i * CW + tc];
+      }
+      part[c] = w;
+      part[A.C + c] = d;
+      const float wt = param<T>(A.weight, g * cpg + c, 1.f);
+      s1 = __builtin_fmaf(d, wt, s1);
+      s2 = __builtin_fmaf(w, wt, s2);
     }
-    part[c] = w;
-    part[A.C + c] = d;
-    const float wt = param<T>(A.weight, g * cpg + c, 1.f);
-    s1 = __builtin_fmaf(d, wt, s1);
-    s2 = __builtin_fmaf(w, wt, s2);
   }
   s1 = wave_sum(s1);
   s2 = wave_sum(s2);
-  if ((threadIdx.x & 63) == 0) {
-    red[0][threadIdx.x >> 6] = s1;
-    red[1][threadIdx.x >> 6] = s2;
+  __syncthreads();
+  if ((tid & 63) == 0) {
+    red[0][tid >> 6] = s1;
+    red[1][tid >> 6] = s2;
   }
   __syncthreads();
-  if (threadIdx.x == 0) {
+  if (tid == 0) {
     const float inv_m = 1.f / ((float)A.L * (float)cpg);
     sums[(b * A.G + g) * 2] = (red[0][0] + red[0][1] + red[0][2] + red[0][3]) * inv_m;
     sums[(b * A.G + g) * 2 + 1] = (red[1][0] + red[1][1] + red[1][2] + red[1][3]) * inv_m;
@@ -481,12 +530,12 @@ template <typename T> __global__ void __launch_bounds__(256) gn_bwd_group_kernel
 
 // third launch: dx, and dw, db from the entries' channel sums
 template <typename T, int V>
-__global__ void __launch_bounds__(256) gn_bwd_dx_kernel(Args A, int splits, const float* sums) {
+__global__ void __launch_bounds__(kThreads) gn_bwd_dx_kernel(Args A, int splits, const float* sums) {
   const int split = blockIdx.x % splits;
   const int64_t b = blockIdx.x / splits;
   const Tile t = make_tile<V>(A, split, splits);
   const int cpg = A.C / A.G;
-  for (int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x; c < A.C; c += (int64_t)gridDim.x * 256) {
+  for (int64_t c = (int64_t)blockIdx.x * kThreads + threadIdx.x; c < A.C; c += (int64_t)gridDim.x * kThreads) {
     float w = 0.f, d = 0.f;
     for (int64_t i = 0; i < A.B; ++i) {
       const float* p = reinterpret_cast<const float*>(A.ws) + i * splits * 2 * A.C + c;
@@ -531,71 +580,80 @@ __global__ void __launch_bounds__(256) gn_bwd_dx_kernel(Args A, int splits, cons
 // ---------------------------------------------------------------------------
 // launches
 // ---------------------------------------------------------------------------
-template <typename T, int V> hipError_t fwd_wave(const Args& a, const Plan& p) {
-  const dim3 grid((unsigned)((a.B * a.G + 3) / 4));
+template <typename T, int V, int K, int NT> void team_launch(const Args& a, const Plan& p, bool bwd) {
+  const int64_t teams = (a.B + p.rows - 1) / p.rows * a.G;
+  const dim3 grid((unsigned)(NT == 64 ? (teams * p.LP + 255) / 256 : teams)), block(NT < 256 ? 256 : NT);
   const hipStream_t st = (hipStream_t)a.stream;
-  switch (p.K) {
-    case 1: hipLaunchKernelGGL((gn_wave_fwd_kernel<T, V, 1>), grid, dim3(256), 0, st, a); break;
-    case 2: hipLaunchKernelGGL((gn_wave_fwd_kernel<T, V, 2>), grid, dim3(256), 0, st, a); break;
-    case 4: hipLaunchKernelGGL((gn_wave_fwd_kernel<T, V, 4>), grid, dim3(256), 0, st, a); break;
-    case 8: hipLaunchKernelGGL((gn_wave_fwd_kernel<T, V, 8>), grid, dim3(256), 0, st, a); break;
-    default:
-      if constexpr (V == 1) hipLaunchKernelGGL((gn_wave_fwd_kernel<T, V, 16>), grid, dim3(256), 0, st, a);
+  // teams of a wave with one load a row and several entries: four entries at a time
+  constexpr int R = NT == 64 && K == 1 ? 4 : 1;
+  if (bwd) {
+    if constexpr (K <= team_loads(V, NT, true)) {
+      if (R > 1 && p.rows > 1) hipLaunchKernelGGL((gn_team_bwd_kernel<T, V, K, NT, R>), grid, block, 0, st, a, p.LP, p.cpv, p.rows);
+      else hipLaunchKernelGGL((gn_team_bwd_kernel<T, V, K, NT, 1>), grid, block, 0, st, a, p.LP, p.cpv, p.rows);
+    }
+  } else if constexpr (K <= team_loads(V, NT, false)) {
+    if (R > 1 && p.rows > 1) hipLaunchKernelGGL((gn_team_fwd_kernel<T, V, K, NT, R>), grid, block, 0, st, a, p.LP, p.cpv, p.rows);
+    else hipLaunchKernelGGL((gn_team_fwd_kernel<T, V, K, NT, 1>), grid, block, 0, st, a, p.LP, p.cpv, p.rows);
   }
+}
+
+template <typename T, int V, int NT> void team_k(const Args& a, const Plan& p, bool bwd) {
+  switch (p.K) {
+    case 1: return team_launch<T, V, 1, NT>(a, p, bwd);
+    case 2: return team_launch<T, V, 2, NT>(a, p, bwd);
+    case 4: return team_launch<T, V, 4, NT>(a, p, bwd);
+    case 8: return team_launch<T, V, 8, NT>(a, p, bwd);
+    default: return team_launch<T, V, 16, NT>(a, p, bwd);
+  }
+}
+
+template <typename T, int V> hipError_t run_team(const Args& a, const Plan& p, bool bwd) {
+  if (p.NT == 64) team_k<T, V, 64>(a, p, bwd);
+  else if (p.NT == 256) team_k<T, V, 256>(a, p, bwd);
+  else team_k<T, V, 1024>(a, p, bwd);
+  if (bwd)
+    hipLaunchKernelGGL(gn_param_kernel<T>, dim3((a.C + 31) / 32), dim3(1024), 0, (hipStream_t)a.stream, a,
+                       (a.B + p.rows - 1) / p.rows);
   return hipGetLastError();
 }
 
 template <typename T, int V> hipError_t fwd_split(const Args& a, const Plan& p) {
-  const int nvec = a.C / V, TX = nvec < 256 ? nvec : 256, TY = 256 / TX;
+  const int nvec = a.C / V, TX = nvec < kThreads ? nvec : kThreads, TY = kThreads / TX;
   const dim3 grid((unsigned)(a.B * p.splits));
   const hipStream_t st = (hipStream_t)a.stream;
-  hipLaunchKernelGGL((gn_stats_kernel<T, V>), grid, dim3(256), (size_t)TY * a.C * 8, st, a, p.splits);
-  hipLaunchKernelGGL((gn_apply_kernel<T, V>), grid, dim3(256), (size_t)a.G * 8, st, a, p.splits);
-  return hipGetLastError();
-}
-
-template <typename T, int V> hipError_t bwd_wave(const Args& a, const Plan& p) {
-  const int64_t parts = (a.B + p.rows - 1) / p.rows;
-  const dim3 grid((unsigned)((parts * a.G + 3) / 4));
-  const hipStream_t st = (hipStream_t)a.stream;
-  const size_t lds = a.L == 1 ? 0 : (size_t)4 * 2 * a.L * (a.C / a.G) * 4;
-  switch (p.K) {
-    case 1: hipLaunchKernelGGL((gn_wave_bwd_kernel<T, V, 1>), grid, dim3(256), lds, st, a, p.rows); break;
-    case 2: hipLaunchKernelGGL((gn_wave_bwd_kernel<T, V, 2>), grid, dim3(256), lds, st, a, p.rows); break;
-    case 4: hipLaunchKernelGGL((gn_wave_bwd_kernel<T, V, 4>), grid, dim3(256), lds, st, a, p.rows); break;
-    default:
-      if constexpr (V == 1) {
-        if (p.K == 8) hipLaunchKernelGGL((gn_wave_bwd_kernel<T, V, 8>), grid, dim3(256), lds, st, a, p.rows);
-        else hipLaunchKernelGGL((gn_wave_bwd_kernel<T, V, 16>), grid, dim3(256), lds, st, a, p.rows);
-      }
-  }
-  hipLaunchKernelGGL(gn_param_kernel<T>, dim3((a.C + 31) / 32), dim3(256), 0, st, a, parts);
+  hipLaunchKernelGGL((gn_stats_kernel<T, V>), grid, dim3(kThreads), (size_t)TY * a.C * 8, st, a, p.splits);
+  hipLaunchKernelGGL((gn_apply_kernel<T, V>), grid, dim3(kThreads), (size_t)a.G * 8, st, a, p.splits);
   return hipGetLastError();
 }
 
 template <typename T, int V> hipError_t bwd_split(const Args& a, const Plan& p) {
-  const int nvec = a.C / V, TX = nvec < 256 ? nvec : 256, TY = 256 / TX;
+  const int nvec = a.C / V, TX = nvec < kThreads ? nvec : kThreads, TY = kThreads / TX;
   const dim3 grid((unsigned)(a.B * p.splits));
   const hipStream_t st = (hipStream_t)a.stream;
   float* sums = reinterpret_cast<float*>(a.ws) + a.B * p.splits * 2 * a.C;
-  hipLaunchKernelGGL((gn_bwd_sums_kernel<T, V>), grid, dim3(256), (size_t)TY * a.C * 8, st, a, p.splits);
+  hipLaunchKernelGGL((gn_bwd_sums_kernel<T, V>), grid, dim3(kThreads), (size_t)TY * a.C * 8, st, a, p.splits);
   hipLaunchKernelGGL((gn_bwd_group_kernel<T>), dim3((unsigned)(a.B * a.G)), dim3(256), 0, st, a, p.splits, sums);
-  hipLaunchKernelGGL((gn_bwd_dx_kernel<T, V>), grid, dim3(256), 0, st, a, p.splits, sums);
+  hipLaunchKernelGGL((gn_bwd_dx_kernel<T, V>), grid, dim3(kThreads), 0, st, a, p.splits, sums);
   return hipGetLastError();
 }
 
-template <typename T> hipError_t fwd_t(const Args& a) {
-  constexpr int F = 16 / sizeof(T);
-  const Plan p = make_plan(a.B, a.L, a.C, a.G, sizeof(T) == 4 ? 0 : 1, a.vec, false);
-  if (p.wave) return p.V == 1 ? fwd_wave<T, 1>(a, p) : fwd_wave<T, F>(a, p);
-  return p.V == 1 ? fwd_split<T, 1>(a, p) : fwd_split<T, F>(a, p);
+template <typename T, int V> hipError_t run_v(const Args& a, const Plan& p, bool bwd) {
+  if (p.team) return run_team<T, V>(a, p, bwd);
+  return bwd ? bwd_split<T, V>(a, p) : fwd_split<T, V>(a, p);
 }
-template <typename T> hipError_t bwd_t(const Args& a) {
-  constexpr int F = 16 / sizeof(T);
-  const Plan p = make_plan(a.B, a.L, a.C, a.G, sizeof(T) == 4 ? 0 : 1, a.vec, true);
-  if (p.wave) return p.V == 1 ? bwd_wave<T, 1>(a, p) : bwd_wave<T, F>(a, p);
-  return p.V == 1 ? bwd_split<T, 1>(a, p) : bwd_split<T, F>(a, p);
+template <typename T> hipError_t run_t(const Args& a, bool bwd) {
+  const Plan p = make_plan(a.B, a.L, a.C, a.G, sizeof(T) == 4 ? 0 : 1, a.vec, bwd);
+  switch (p.V) {
+    case 1: return run_v<T, 1>(a, p, bwd);
+    case 2: return run_v<T, 2>(a, p, bwd);
+    case 4: return run_v<T, 4>(a, p, bwd);
+    default:
+      if constexpr (sizeof(T) == 2) return run_v<T, 8>(a, p, bwd);
+      return hipErrorInvalidValue;
+  }
 }
+template <typename T> hipError_t fwd_t(const Args& a) { return run_t<T>(a, false); }
+template <typename T> hipError_t bwd_t(const Args& a) { return run_t<T>(a, true); }
 
 }  // namespace gn
 }  // namespace gspn

@@ -393,7 +393,7 @@ size_t fwd_workspace(int64_t B, int64_t L, int C, int G, int dtype) {
   size_t most = 0;
   for (int vec = 0; vec < 2; ++vec) {
     const Plan p = make_plan(B, L, C, G, dtype, vec, false);
-    const size_t n = p.wave ? 0 : round256((size_t)B * p.splits * G * 8);
+    const size_t n = p.team ? 0 : round256((size_t)B * p.splits * G * 8);
     most = n > most ? n : most;
   }
   return most;
@@ -402,7 +402,7 @@ size_t bwd_workspace(int64_t B, int64_t L, int C, int G, int dtype) {
   size_t most = 0;
   for (int vec = 0; vec < 2; ++vec) {
     const Plan p = make_plan(B, L, C, G, dtype, vec, true);
-    const size_t n = p.wave ? (size_t)((B + p.rows - 1) / p.rows) * 2 * C * 4
+    const size_t n = p.team ? (size_t)((B + p.rows - 1) / p.rows) * 2 * C * 4
                             : (size_t)B * p.splits * 2 * C * 4 + (size_t)B * G * 8;
     most = n > most ? n : most;
   }
