@@ -47,11 +47,21 @@ __device__ __forceinline__ float act_slope(float z, int act) {
   return 1.f;
 }
 
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int k = 1; k < 64; k <<= 1) v += __shfl_xor(v, k);
+// sums over neighbouring lanes, in every lane: 2, 4, 8 and 16 lanes by moves
+// within a row of 16 (no trip through LDS), 32 and 64 by shuffles
+template <int CTRL> __device__ __forceinline__ float dpp_add(float v) {
+  return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float lanes_sum(float v, int lanes) {
+  if (lanes > 1) v = dpp_add<0xB1>(v);   // the other of two
+  if (lanes > 2) v = dpp_add<0x4E>(v);   // the other two of four
+  if (lanes > 4) v = dpp_add<0x141>(v);  // mirrored within eight
+  if (lanes > 8) v = dpp_add<0x140>(v);  // mirrored within sixteen
+  if (lanes > 16) v += __shfl_xor(v, 16);
+  if (lanes > 32) v += __shfl_xor(v, 32);
   return v;
 }
+__device__ __forceinline__ float wave_sum(float v) { return lanes_sum(v, 64); }
 
 // mean and 1 / sqrt(var + eps) from the sums of x - p and (x - p)^2 over m values
 __device__ __forceinline__ void finish_stats(float p, float s, float q, float inv_m, float eps, float& mean,
@@ -101,8 +111,7 @@ template <int V, int K, int NT> struct Team {
 // sum over a team, in every thread of it; `red`: NT / 64 floats
 template <int NT> __device__ __forceinline__ float team_sum(float v, int LP, float* red) {
   if constexpr (NT == 64) {
-    for (int k = 1; k < LP; k <<= 1) v += __shfl_xor(v, k);
-    return v;
+    return lanes_sum(v, LP);
   } else {
     v = wave_sum(v);
     __syncthreads();
@@ -416,8 +425,9 @@ template <typename T, int V> __global__ void __launch_bounds__(kThreads) gn_appl
       a[j] = st[A.G + g] * param<T>(A.weight, ch, 1.f);
       c[j] = param<T>(A.bias, ch, 0.f);
     }
+    // last rows first: they are the ones that the first launch left in this die's L2
 #pragma unroll 4
-    for (int64_t r = t.r0 + t.ty; r < t.r1; r += t.TY) {
+    for (int64_t r = t.r1 - 1 - t.ty; r >= t.r0; r -= t.TY) {
       float v[V];
       load_v<T, V>(x + r * A.C + cv * V, v);
 #pragma unroll
@@ -561,8 +571,9 @@ __global__ void __launch_bounds__(kThreads) gn_bwd_dx_kernel(Args A, int splits,
       s1[j] = sums[g * 2];
       s2[j] = sums[g * 2 + 1];
     }
+    // last rows first, as in the forward's second launch
 #pragma unroll 2
-    for (int64_t r = t.r0 + t.ty; r < t.r1; r += t.TY) {
+    for (int64_t r = t.r1 - 1 - t.ty; r >= t.r0; r -= t.TY) {
       float v[V], d[V];
       load_v<T, V>(x + r * A.C + cv * V, v);
       load_v<T, V>(dy + r * A.C + cv * V, d);
