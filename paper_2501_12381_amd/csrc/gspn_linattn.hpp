@@ -34,7 +34,7 @@ struct FwdArgs {
   float* sf;              // final states, or null
   const float* start;     // start states of pieces that are not their sequence's first (register order)
   void* o;                // (B, T, H, Dv)
-  int ovec;               // o's rows can be written four values at a time
+  int ovec;               // o's rows are whole 16-byte vectors
   void* stream;
 };
 hipError_t linattn_fwd_f32(const FwdArgs& a);
@@ -53,6 +53,7 @@ struct StateArgs {
   int per_token;
   float scale;
   int reverse;
+  int exact;               // the state is returned: all its bits
   // mode 0: pieces that are not their sequence's last (reverse: first), from a zero
   // state: the state at the piece's end to `local`, its decay to `gtot`.
   // mode 1: every piece from its start state (s0 or `local`): the state before
@@ -91,7 +92,7 @@ struct BwdArgs {
   const float* end;        // end-state gradients of pieces that are not their sequence's last
   const void* chunks;      // state before each chunk (x = v, y = k)
   void *dq, *dk, *dv;      // dq, dk: (B, T, Hk, Dk) when H == Hk, else null
-  int dkvec, dvvec;        // their rows can be written four values at a time
+  int dkvec, dvvec;        // their rows are whole 16-byte vectors
   float *dq32, *dk32;      // (B, T, H, Dk) when H != Hk
   void* da;                // per_token: (B, T, H)
   float* da_piece;         // else: pieces x H sums

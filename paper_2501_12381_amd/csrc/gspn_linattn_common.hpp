@@ -35,15 +35,25 @@ typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 // element types: chunk length, LDS row padding, matrix products
 // ---------------------------------------------------------------------------
 // A fragment is the 8 values a lane gives to one product step of depth 16: lane
-// l holds line l % 32 of its operand and, with h = l / 32, the depths 8h..8h+7.
-// Any order of the depths serves as long as both operands have the same one.
+// l holds line pl(l) of its 32-line operand and, with h = l / 32, the depths
+// 8h..8h+7.  pl swaps the middle fours of every sixteen lines: register r of half
+// h of a 32 x 32 result is row 8 (r/4) + 4h + r%4 of the first operand's lanes, so
+// with that order it is line 16 (r/8) + 8h + r%8.  A lane then holds runs of 8
+// neighbouring lines: 8 registers of a result are a fragment of the next product
+// as they are, and 16 bytes of a row in LDS or global memory.
+__device__ __forceinline__ int pl(int lane) { return (lane & 0x13) | ((lane & 4) << 1) | ((lane & 8) >> 1); }
+__device__ __forceinline__ int reg_line(int r, int h) { return 16 * (r >> 3) + 8 * h + (r & 7); }
+
 template <typename T> struct Elem;
 
 template <> struct Elem<bf16> {
   static constexpr int kChunk = 64;
-  static constexpr int kVec = 8;   // elements of a 16-byte load
-  static constexpr int kPad = 8;   // LDS rows are 16 bytes longer: 16 rows cover all 64 banks
-  // an fp32 value as sums of bf16 ones: three carry all of its 24 bits
+  static constexpr int kVec = 8;  // elements of a 16-byte load
+  // LDS rows in 16-byte slots, against the 16 slots that the banks make: an odd
+  // multiple apart for rows read along (8 lanes, 8 rows) and such that two
+  // neighbouring slots of four rows differ, for reads down columns
+  static constexpr int stride(int n) { return n + (n % 128 == 0 ? 24 : 8); }
+  // an fp32 value as a sum of bf16 ones: three carry all of its 24 bits, two 16
   static constexpr int kParts = 3;
   struct Frag {
     bf16x8 v;
@@ -56,50 +66,51 @@ template <> struct Elem<bf16> {
 #pragma unroll
     for (int j = 0; j < 8; ++j) x[j] = (float)f.v[j];
   }
-  // x = sum of the parts, each the rounding of what the ones before left
-  static __device__ __forceinline__ void split(const float* x, Frag* f) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      float r = x[j];
-#pragma unroll
-      for (int p = 0; p < kParts; ++p) {
-        const bf16 b = (bf16)r;
-        f[p].v[j] = b;
-        r -= (float)b;
-      }
+  // x = f[0] + f[1] (+ f[2]): upper halves cut off, the last part rounded
+  static __device__ __forceinline__ void split(const float* x, Frag* f, bool three) {
+    float r[8];
+    cut(x, f[0], r);
+    if (three) {
+      float q[8];
+      cut(r, f[1], q);
+      set(f[2], q);
+    } else {
+      set(f[1], r);
     }
+  }
+  static __device__ __forceinline__ void cut(const float* x, Frag& f, float* rest) {
+    uint32_t w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t a = __float_as_uint(x[2 * j]), b = __float_as_uint(x[2 * j + 1]);
+      w[j] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+      rest[2 * j] = x[2 * j] - __uint_as_float(a & 0xffff0000u);
+      rest[2 * j + 1] = x[2 * j + 1] - __uint_as_float(b & 0xffff0000u);
+    }
+    f.v = __builtin_bit_cast(bf16x8, w);
   }
   static __device__ __forceinline__ void mma(f32x16& c, const Frag& a, const Frag& b) {
     c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, b.v, c, 0, 0, 0);
   }
-  // 8 consecutive values at p (16-byte aligned) / two runs of 4
   static __device__ __forceinline__ Frag row(const bf16* p) { return {*reinterpret_cast<const bf16x8*>(p)}; }
-  static __device__ __forceinline__ Frag row2(const bf16* p, const bf16* q) {
-    const bf16x4 a = *reinterpret_cast<const bf16x4*>(p), b = *reinterpret_cast<const bf16x4*>(q);
-    return {__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7)};
-  }
-  // 8 values down a column of an LDS tile: rows r0..r0+3 and r1..r1+3 (both
-  // the lane's own), columns c0..c0+31, column l % 32 for this lane.  The
-  // transposing read hands lane i of 16 the values of column i from four rows,
-  // when lane i addresses four values of row i / 4, columns 4 (i % 4).
-  static __device__ __forceinline__ Frag col(const bf16* tile, int stride, int r0, int r1, int c0, int lane) {
-    const int i = lane & 15;
-    const bf16* p = tile + (r0 + (i >> 2)) * stride + c0 + (lane & 16) + 4 * (i & 3);
-    const bf16* q = tile + (r1 + (i >> 2)) * stride + c0 + (lane & 16) + 4 * (i & 3);
+  // 8 values down a column of an LDS tile: rows r..r+7 (r the lane's own), column
+  // c0 + pl(lane).  The transposing read hands lane i of 16 the values that the
+  // lanes 4j + i/4 address at place i % 4, j = 0..3: lane i addresses row i / 4, and
+  // the order of the fours of columns is pl's.
+  static __device__ __forceinline__ Frag col(const bf16* tile, int stride, int r, int c0, int lane) {
+    const int i = lane & 15, c = ((lane & 1) << 3) | ((lane & 2) << 1);  // columns 0, 8, 4, 12
+    const bf16* p = tile + (r + (i >> 2)) * stride + c0 + (lane & 16) + c;
     const bf16x4 a = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p));
-    const bf16x4 b = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)q));
+    const bf16x4 b = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 4 * stride)));
     return {__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7)};
   }
-  static __device__ __forceinline__ void store4(bf16* p, const float* x) {
-    uint2 w;
+  static __device__ __forceinline__ void store8(bf16* p, const float* x) {
+    uint4 w;
     w.x = pack_bf2(x[0], x[1]);
     w.y = pack_bf2(x[2], x[3]);
-    *reinterpret_cast<uint2*>(p) = w;
-  }
-  static __device__ __forceinline__ void load4(const bf16* p, float* x) {
-    const bf16x4 v = *reinterpret_cast<const bf16x4*>(p);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] = (float)v[j];
+    w.z = pack_bf2(x[4], x[5]);
+    w.w = pack_bf2(x[6], x[7]);
+    *reinterpret_cast<uint4*>(p) = w;
   }
 };
 
@@ -108,7 +119,7 @@ template <> struct Elem<float> {
   // state at 64, and the fp32 matrix rate is a sixteenth of bf16's
   static constexpr int kChunk = 32;
   static constexpr int kVec = 4;
-  static constexpr int kPad = 4;
+  static constexpr int stride(int n) { return n + 4; }
   static constexpr int kParts = 1;
   struct Frag {
     float v[8];
@@ -121,64 +132,43 @@ template <> struct Elem<float> {
 #pragma unroll
     for (int j = 0; j < 8; ++j) x[j] = f.v[j];
   }
-  static __device__ __forceinline__ void split(const float* x, Frag* f) { set(f[0], x); }
+  static __device__ __forceinline__ void split(const float* x, Frag* f, bool) { set(f[0], x); }
   static __device__ __forceinline__ void mma(f32x16& c, const Frag& a, const Frag& b) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[j], b.v[j], c, 0, 0, 0);
   }
-  static __device__ __forceinline__ Frag row2(const float* p, const float* q) {
-    const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(q);
+  static __device__ __forceinline__ Frag row(const float* p) {
+    const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
     return {{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
   }
-  static __device__ __forceinline__ Frag row(const float* p) { return row2(p, p + 4); }
-  static __device__ __forceinline__ Frag col(const float* tile, int stride, int r0, int r1, int c0, int lane) {
+  static __device__ __forceinline__ Frag col(const float* tile, int stride, int r, int c0, int lane) {
     Frag f;
-    const float* p = tile + c0 + (lane & 31);
+    const float* p = tile + r * stride + c0 + pl(lane & 31);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      f.v[j] = p[(r0 + j) * stride];
-      f.v[4 + j] = p[(r1 + j) * stride];
-    }
+    for (int j = 0; j < 8; ++j) f.v[j] = p[j * stride];
     return f;
   }
-  static __device__ __forceinline__ void store4(float* p, const float* x) {
+  static __device__ __forceinline__ void store8(float* p, const float* x) {
     *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
-  }
-  static __device__ __forceinline__ void load4(const float* p, float* x) {
-    const float4 v = *reinterpret_cast<const float4*>(p);
-    x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+    *reinterpret_cast<float4*>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
   }
 };
 
-// Depth orders of a fragment in block k0 of 16: natural (8h..8h+7), and the one
-// in which the registers of a 32 x 32 result hold its rows: register r of half h
-// is row 8 (r/4) + 4h + r%4, so registers 0-7 are rows 4h..4h+3, 8+4h..8+4h+3.
+// depths k0..k0+15 of line `row` of an LDS tile, along the row; and of column
+// c0 + pl(lane), down the rows
 template <typename T>
 __device__ __forceinline__ typename Elem<T>::Frag row_frag(const T* tile, int stride, int row, int k0, int h) {
   return Elem<T>::row(tile + row * stride + k0 + 8 * h);
 }
 template <typename T>
-__device__ __forceinline__ typename Elem<T>::Frag row_frag_acc(const T* tile, int stride, int row, int k0, int h) {
-  const T* p = tile + row * stride + k0 + 4 * h;
-  return Elem<T>::row2(p, p + 8);
-}
-template <typename T>
 __device__ __forceinline__ typename Elem<T>::Frag col_frag(const T* tile, int stride, int k0, int c0, int lane) {
-  const int r = k0 + 8 * (lane >> 5);
-  return Elem<T>::col(tile, stride, r, r + 4, c0, lane);
+  return Elem<T>::col(tile, stride, k0 + 8 * (lane >> 5), c0, lane);
 }
-template <typename T>
-__device__ __forceinline__ typename Elem<T>::Frag col_frag_acc(const T* tile, int stride, int k0, int c0, int lane) {
-  const int r = k0 + 4 * (lane >> 5);
-  return Elem<T>::col(tile, stride, r, r + 8, c0, lane);
-}
-__device__ __forceinline__ int acc_row(int r, int h) { return 8 * (r >> 2) + 4 * h + (r & 3); }
-
-// the fragment that 8 registers (kk even: 0-7, odd: 8-15) of a result tile are
-template <typename T> __device__ __forceinline__ typename Elem<T>::Frag acc_frag(const f32x16& s, int odd) {
+// the fragment of depths 16 kk..16 kk + 15 that two results' registers (32 lines each) are
+template <typename T> __device__ __forceinline__ typename Elem<T>::Frag reg_frag(const f32x16* s, int kk) {
   float x[8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) x[j] = s[8 * odd + j];
+  for (int j = 0; j < 8; ++j) x[j] = s[kk >> 1][8 * (kk & 1) + j];
   typename Elem<T>::Frag f;
   Elem<T>::set(f, x);
   return f;
@@ -253,52 +243,74 @@ __device__ __forceinline__ Piece find_piece(const Geom& g, int i) {
 // ---------------------------------------------------------------------------
 // staging: a chunk's rows from global memory to registers to LDS
 // ---------------------------------------------------------------------------
-// C rows of D <= DP values; rows past `rows` and columns past D are zero.
+// C rows of D <= DP values; rows past the piece and columns past D are zero.
 template <typename T, int DP, int NT> struct Stage {
   static constexpr int C = Elem<T>::kChunk, V = Elem<T>::kVec;
-  static constexpr int kStride = DP + Elem<T>::kPad;
+  static constexpr int kStride = Elem<T>::stride(DP);
   static constexpr int kRowVecs = DP / V;
-  static constexpr int kPer = (C * kRowVecs + NT - 1) / NT;
-  static constexpr bool kExact = C * kRowVecs % NT == 0;
+  static constexpr int kRows = NT / kRowVecs;  // rows of one load of all threads
+  static constexpr int kPer = (C + kRows - 1) / kRows;
+  static_assert(NT % kRowVecs == 0, "");
   uint4 r[kPer];
+  const T* p;        // this thread's place in its first row of the next chunk
+  int64_t step;      // elements between its rows
+  int row, c, D;
+  bool vec;
 
-  __device__ __forceinline__ void load(const T* __restrict__ base, int64_t tstride, int rows, int D, bool vec,
-                                       int tid) {
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int p = tid + i * NT, row = p / kRowVecs, c = (p % kRowVecs) * V;
-      uint4 x = make_uint4(0, 0, 0, 0);
-      if ((kExact || row < C) && row < rows && c < D) {
-        const T* s = base + row * tstride + c;
-        if (vec) {
-          x = *reinterpret_cast<const uint4*>(s);
-        } else {  // rows that are not whole 16-byte vectors
-          T e[V];
-#pragma unroll
-          for (int j = 0; j < V; ++j) e[j] = c + j < D ? s[j] : (T)0.f;
-          x = __builtin_bit_cast(uint4, e);
-        }
-      }
-      r[i] = x;
-    }
+  // t0: the first chunk's first row
+  __device__ __forceinline__ void init(const T* base, const Rows& rows, int size, int t0, int tid) {
+    row = tid / kRowVecs;
+    c = (tid % kRowVecs) * V;
+    D = size;
+    vec = rows.vec;
+    p = base + (t0 + row) * rows.st + c;
+    step = kRows * rows.st;
   }
-  __device__ __forceinline__ void store(T* tile, int tid) const {
+  // left: rows of the piece from the chunk's first one on; then `dir` chunks further
+  __device__ __forceinline__ void load(int left, const Rows& rows, int dir) {
+    if (vec && left >= C && D == DP && C % kRows == 0) {
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int p = tid + i * NT, row = p / kRowVecs, c = (p % kRowVecs) * V;
-      if (kExact || row < C) *reinterpret_cast<uint4*>(tile + row * kStride + c) = r[i];
+      for (int i = 0; i < kPer; ++i) r[i] = *reinterpret_cast<const uint4*>(p + i * step);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const int at = row + i * kRows;
+        uint4 x = make_uint4(0, 0, 0, 0);
+        if (at < C && at < left && c < D) {
+          const T* s = p + i * step;
+          if (vec) {
+            x = *reinterpret_cast<const uint4*>(s);
+          } else {  // rows that are not whole 16-byte vectors
+            T e[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j) e[j] = c + j < D ? s[j] : (T)0.f;
+            x = __builtin_bit_cast(uint4, e);
+          }
+        }
+        r[i] = x;
+      }
     }
+    p += dir * (C * rows.st);
+  }
+  __device__ __forceinline__ void store(T* tile) const {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      if (C % kRows == 0 || row + i * kRows < C)
+        *reinterpret_cast<uint4*>(tile + (row + i * kRows) * kStride + c) = r[i];
   }
 };
 
 // ---------------------------------------------------------------------------
 // a chunk's decays
 // ---------------------------------------------------------------------------
-// G_t in powers of two, summed in 64 bits and held as two floats, so that
-// differences keep their digits behind a token whose decay is a reset (-inf,
-// taken as 2^-150: zero in fp32).
-template <int C> struct Decays {
-  float hi[C], lo[C];  // G_t
+// G_t in powers of two, summed in 64 bits.  In fp32 it is kept as two floats, so
+// that differences keep their digits behind a token whose decay is a reset (-inf,
+// taken as 2^-150: zero in fp32); in bf16 one float's are enough for P and Z, which
+// are rounded to bf16.
+template <typename T> struct Decays {
+  static constexpr int C = Elem<T>::kChunk;
+  float hi[C];         // G_t
+  float lo[C];
   float qf[C];         // scale e^{G_t}
   float kf[C];         // e^{G_C - G_t}
   float tot;           // e^{G_C}
@@ -313,7 +325,8 @@ __device__ __forceinline__ double load_decay(const T* __restrict__ a, int64_t st
 }
 
 // one wave; g: lane t's own term (0 past the chunk).  Returns G_C.
-template <int C> __device__ __forceinline__ double chunk_decays(Decays<C>& d, double g, float scale, int lane) {
+template <typename T> __device__ __forceinline__ double chunk_decays(Decays<T>& d, double g, float scale, int lane) {
+  constexpr int C = Elem<T>::kChunk;
 #pragma unroll
   for (int k = 1; k < C; k <<= 1) {
     const double o = __shfl_up(g, k);
@@ -331,9 +344,157 @@ template <int C> __device__ __forceinline__ double chunk_decays(Decays<C>& d, do
   return all;
 }
 
-// e^{G_t - G_s} for s <= t, 0 above
-template <int C> __device__ __forceinline__ float decay_between(const Decays<C>& d, int s, float hi_t, float lo_t) {
-  return exp2_hw((hi_t - d.hi[s]) + (lo_t - d.lo[s]));
+// x[j] = raw[j] scale e^{G_t - G_{s+j}} for s + j <= t, 0 above
+template <typename T, int N>
+__device__ __forceinline__ void decayed(const Decays<T>& d, const float* raw, float scale, int t, int s, float* x) {
+  const float hi = d.hi[t], lo = sizeof(T) == 4 ? d.lo[t] : 0.f;
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    float e = hi - d.hi[s + j];
+    if constexpr (sizeof(T) == 4) e += lo - d.lo[s + j];
+    x[j] = s + j <= t ? raw[j] * (scale * exp2_hw(e)) : 0.f;
+  }
+}
+
+// The products of a chunk's token pairs, decayed: out[t][s] = (a_s . b_t) scale
+// e^{G_t - G_s} for s <= t, 0 above; the work of `waves` waves, of which this is
+// number `wave`.  Three of four quarters of the C x C table: bf16 quarters are 32 x 32
+// tiles, and the one above the diagonal is never read; fp32 ones are 16 x 16
+// (a quarter of the time of one wave's 32 x 32 tile), and the fourth is zeros.
+template <typename T, int DP>
+__device__ __forceinline__ void pair_table(const Decays<T>& d, const T* a, const T* b, int stride, float scale, T* out,
+                                           int ostride, int wave, int waves, int lane) {
+  constexpr int Q = Elem<T>::kChunk / 2;
+  for (int tile = wave; tile < (sizeof(T) == 2 ? 3 : 4); tile += waves) {
+    const int tt = tile == 3 ? 0 : (tile + 1) >> 1, st = tile == 3 ? 1 : tile >> 1;  // (t, s): 00, 10, 11, (01)
+    if constexpr (sizeof(T) == 2) {
+      const int h = lane >> 5, l = pl(lane & 31);
+      f32x16 acc = {};
+#pragma unroll
+      for (int k0 = 0; k0 < DP; k0 += 16)
+        Elem<T>::mma(acc, row_frag(a, stride, Q * st + l, k0, h), row_frag(b, stride, Q * tt + l, k0, h));
+      const int t = Q * tt + l;
+#pragma unroll
+      for (int r = 0; r < 16; r += 8) {
+        const int s = Q * st + reg_line(r, h);
+        float raw[8], x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) raw[j] = acc[r + j];
+        decayed<T, 8>(d, raw, scale, t, s, x);
+        Elem<T>::store8(out + t * ostride + s, x);
+      }
+    } else {
+      typedef float f32x4 __attribute__((ext_vector_type(4)));
+      const int l = lane & 15, q = lane >> 4, t = Q * tt + l, s = Q * st + 4 * q;
+      float x[4] = {0.f, 0.f, 0.f, 0.f};
+      if (tile < 3) {
+        f32x4 acc = {};
+#pragma unroll
+        for (int k0 = 0; k0 < DP; k0 += 32) {
+          const auto fa = Elem<T>::row(a + (Q * st + l) * stride + k0 + 8 * q),
+                     fb = Elem<T>::row(b + (Q * tt + l) * stride + k0 + 8 * q);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(fa.v[j], fb.v[j], acc, 0, 0, 0);
+        }
+        const float raw[4] = {acc[0], acc[1], acc[2], acc[3]};
+        decayed<T, 4>(d, raw, scale, t, s, x);
+      }
+      *reinterpret_cast<float4*>(out + t * ostride + s) = make_float4(x[0], x[1], x[2], x[3]);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// a state in registers: tiles of 32 lines x along the registers, one wave's 32 lines
+// y along the lanes
+// ---------------------------------------------------------------------------
+// state = tot state + sum_t x_t (f_t y_t)^T over a chunk.  y's values are scaled
+// in fp32 and given to the product in parts (Elem::split): two keep 16 bits, enough
+// for a state that only bf16 outputs are made of, three all 24, for one that is
+// returned (2 parts leave it 3e-6 off, one 2e-3).
+template <typename T, int XP>
+__device__ __forceinline__ void state_add(f32x16* S, const T* x, int xstride, const T* y, int ystride, int ycol,
+                                          const float* f, float tot, bool three, int lane) {
+  constexpr int C = Elem<T>::kChunk, NP = Elem<T>::kParts;
+  const int h = lane >> 5;
+#pragma unroll
+  for (int m = 0; m < XP / 32; ++m) S[m] *= tot;
+#pragma unroll
+  for (int k0 = 0; k0 < C; k0 += 16) {
+    float v[8];
+    Elem<T>::get(col_frag(y, ystride, k0, ycol, lane), v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] *= f[k0 + 8 * h + j];
+    typename Elem<T>::Frag p[NP];
+    Elem<T>::split(v, p, three);
+#pragma unroll
+    for (int m = 0; m < XP / 32; ++m) {
+      const auto xf = col_frag(x, xstride, k0, 32 * m, lane);
+      Elem<T>::mma(S[m], xf, p[0]);
+      if constexpr (NP > 1) {
+        Elem<T>::mma(S[m], xf, p[1]);
+        if (three) Elem<T>::mma(S[m], xf, p[2]);
+      }
+    }
+  }
+}
+
+// S from / to (x, y)-strided fp32 memory (null: zero); y: this lane's line
+template <int XP>
+__device__ __forceinline__ void state_read(f32x16* S, const float* s, int Dx, int Dy, int sx, int sy, int y, int h) {
+#pragma unroll
+  for (int m = 0; m < XP / 32; ++m)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int x = 32 * m + reg_line(r, h);
+      S[m][r] = s && x < Dx && y < Dy ? s[x * sx + y * sy] : 0.f;
+    }
+}
+template <int XP>
+__device__ __forceinline__ void state_write(const f32x16* S, float* s, int Dx, int Dy, int sx, int sy, int y, int h) {
+#pragma unroll
+  for (int m = 0; m < XP / 32; ++m)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int x = 32 * m + reg_line(r, h);
+      if (x < Dx && y < Dy) s[x * sx + y * sy] = S[m][r];
+    }
+}
+// register order: register after register, 64 lanes each
+template <int XP> __device__ __forceinline__ void state_read_regs(f32x16* S, const float* s, int wave, int lane) {
+#pragma unroll
+  for (int m = 0; m < XP / 32; ++m)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) S[m][r] = s[((wave * (XP / 32) + m) * 16 + r) * 64 + lane];
+}
+template <int XP> __device__ __forceinline__ void state_write_regs(const f32x16* S, float* s, int wave, int lane) {
+#pragma unroll
+  for (int m = 0; m < XP / 32; ++m)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[((wave * (XP / 32) + m) * 16 + r) * 64 + lane] = S[m][r];
+}
+
+// the two runs of 8 lines that a result's registers are, to a row at p (line 0 of
+// the tile); left: lines of the tile that the row has; vec: whole runs, p aligned
+template <typename T> __device__ __forceinline__ void put_lines(T* p, const f32x16& acc, int left, int vec, int h) {
+#pragma unroll
+  for (int r = 0; r < 16; r += 8) {
+    const int c = reg_line(r, h);
+    float x[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = acc[r + j];
+    if (vec) {
+      if (c < left) Elem<T>::store8(p + c, x);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (c + j < left) p[c + j] = from_f<T>(x[j]);
+    }
+  }
+}
+
+template <typename T> __device__ __forceinline__ const T* head_rows(const Rows& r, const Piece& pc, int head) {
+  return reinterpret_cast<const T*>(r.p) + pc.batch * r.sb + (int64_t)pc.t0 * r.st + (int64_t)head * r.sh;
 }
 
 }  // namespace la

@@ -1,4 +1,5 @@
 // Linear attention, forward and the walks of the state, bf16 tensors.
+#include "gspn_linattn_fwd_impl.hpp"
 #include "gspn_linattn_state_impl.hpp"
 
 namespace gspn {

@@ -8,19 +8,19 @@
 // wave's 64 lanes each): it would round them to that type all the same.
 #pragma once
 
-#include "gspn_linattn_fwd_impl.hpp"
+#include "gspn_linattn_common.hpp"
 
 namespace gspn {
 namespace la {
 
 template <typename T, int XP, int YP> __global__ void __launch_bounds__(2 * YP, 2) linattn_state_kernel(StateArgs A) {
   constexpr int C = Elem<T>::kChunk, NT = 2 * YP;
-  constexpr int XS = XP + Elem<T>::kPad, YS = YP + Elem<T>::kPad;
+  constexpr int XS = Elem<T>::stride(XP), YS = Elem<T>::stride(YP);
   __shared__ __align__(16) T sx[C * XS], sy[C * YS];
-  __shared__ Decays<C> dec;
+  __shared__ Decays<T> dec;
 
   const Geom& g = A.g;
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, h = lane >> 5, l = lane & 31;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, h = lane >> 5, l = pl(lane & 31);
   const int head = blockIdx.x % g.H, pi = blockIdx.x / g.H;
   const Piece pc = find_piece(g, pi);
   if (pc.len < 0 || pc.seq >= g.N) return;
@@ -37,40 +37,39 @@ template <typename T, int XP, int YP> __global__ void __launch_bounds__(2 * YP, 
   } else {
     state_read_regs<XP>(S, A.local + slot * (XP * YP), wave, lane);
   }
-  const T *x = head_rows<T>(A.x, pc, A.x_shared ? hk : head), *y = head_rows<T>(A.y, pc, A.y_shared ? hk : head);
   const T* a = reinterpret_cast<const T*>(A.a) + head +
                (A.per_token ? (pc.batch * g.T + pc.t0) * (int64_t)g.H : (int64_t)0);
   const int64_t at = A.per_token ? g.H : 0;
 
   Stage<T, XP, NT> rx;
   Stage<T, YP, NT> ry;
+  const int n = (pc.len + C - 1) / C, dir = A.reverse ? -1 : 1, from = A.reverse && n > 0 ? (n - 1) * C : 0;
+  rx.init(head_rows<T>(A.x, pc, A.x_shared ? hk : head), A.x, A.Dx, from, tid);
+  ry.init(head_rows<T>(A.y, pc, A.y_shared ? hk : head), A.y, A.Dy, from, tid);
   double ra = 0.0, all = 0.0;
   const auto load = [&](int t) {
-    const int rows = pc.len - t;
-    rx.load(x + t * A.x.st, A.x.st, rows, A.Dx, A.x.vec, tid);
-    ry.load(y + t * A.y.st, A.y.st, rows, A.Dy, A.y.vec, tid);
-    if (wave == 0 && lane < C) ra = load_decay(a + t * at, at, lane, rows);
+    const int left = pc.len - t;
+    rx.load(left, A.x, dir);
+    ry.load(left, A.y, dir);
+    if (wave == 0 && lane < C) ra = load_decay(a + t * at, at, lane, left);
   };
-  const int n = (pc.len + C - 1) / C;
   T* chunks = reinterpret_cast<T*>(A.chunks);
   const float* f = A.reverse ? dec.qf : dec.kf;
-  if (n > 0) load((A.reverse ? n - 1 : 0) * C);
+  if (n > 0) load(from);
   for (int i = 0; i < n; ++i) {
     const int c = A.reverse ? n - 1 - i : i;
-    rx.store(sx, tid);
-    ry.store(sy, tid);
+    rx.store(sx);
+    ry.store(sy);
     if (wave == 0) all += chunk_decays(dec, ra, A.scale, lane);
     lds_barrier();
-    if (i + 1 < n) load((A.reverse ? c - 1 : c + 1) * C);
+    if (i + 1 < n) load((c + dir) * C);
     if (A.mode == 1) {
       T* out = chunks + (((int64_t)pi * (g.L / C) + c) * g.H + head) * (XP * YP) + (wave * (XP / 16) * 64 + lane) * 8;
 #pragma unroll
-      for (int kk = 0; kk < XP / 16; ++kk) {
-        const auto fr = acc_frag<T>(S[kk >> 1], kk & 1);
-        *reinterpret_cast<typename Elem<T>::Frag*>(out + kk * 512) = fr;
-      }
+      for (int kk = 0; kk < XP / 16; ++kk)
+        *reinterpret_cast<typename Elem<T>::Frag*>(out + kk * 512) = reg_frag<T>(S, kk);
     }
-    state_add<T, XP>(S, sx, XS, sy, YS, 32 * wave, f, dec.tot, lane);
+    state_add<T, XP>(S, sx, XS, sy, YS, 32 * wave, f, dec.tot, A.exact, lane);
     lds_barrier();
   }
   if (A.mode == 0) {

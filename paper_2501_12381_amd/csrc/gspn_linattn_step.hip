@@ -109,7 +109,7 @@ __global__ void __launch_bounds__(256) linattn_join_kernel(JoinArgs A, int XP, i
   if (first == last) return;
   const int e = (blockIdx.x % parts) * 256 + threadIdx.x;  // register order: wave (y / 32), tile (x / 32), register, lane
   const int lane = e & 63, r = (e >> 6) & 15, m = (e >> 10) % (XP / 32), w = (e >> 10) / (XP / 32);
-  const int x = 32 * m + acc_row(r, lane >> 5), y = 32 * w + (lane & 31);
+  const int x = 32 * m + reg_line(r, lane >> 5), y = 32 * w + pl(lane & 31);
   const int64_t size = (int64_t)XP * YP;
   float run = A.s0 && x < A.Dx && y < A.Dy
                   ? A.s0[((int64_t)n * g.H + head) * A.Dx * A.Dy + x * A.sx + y * A.sy] : 0.f;
@@ -126,18 +126,26 @@ __global__ void __launch_bounds__(256) linattn_join_kernel(JoinArgs A, int XP, i
 // ---------------------------------------------------------------------------
 // sums over the value heads of a query/key head, and over the pieces
 // ---------------------------------------------------------------------------
-template <typename T> __global__ void __launch_bounds__(256) linattn_share_kernel(ReduceArgs A) {
-  const int64_t n = A.tokens * A.Hk * A.Dk;
-  const int group = A.H / A.Hk;
+// V values a thread; a workgroup takes whole rows (a token and query/key head each)
+template <typename T, int V> __global__ void __launch_bounds__(256) linattn_share_kernel(ReduceArgs A) {
+  const int group = A.H / A.Hk, nv = A.Dk / V, per = 256 / nv, r = threadIdx.x / nv, d = (threadIdx.x - r * nv) * V;
   const float* in = blockIdx.y ? A.dk32 : A.dq32;
   T* out = reinterpret_cast<T*>(blockIdx.y ? A.dk : A.dq);
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-    const int64_t th = i / A.Dk;  // token and query/key head
-    const int d = (int)(i - th * A.Dk);
-    const float* p = in + th * group * A.Dk + d;
-    float t = p[0];
-    for (int j = 1; j < group; ++j) t += p[(int64_t)j * A.Dk];
-    out[i] = from_f<T>(t);
+  const int64_t rows = A.tokens * A.Hk;
+  if (r >= per) return;
+  for (int64_t row = (int64_t)blockIdx.x * per + r; row < rows; row += (int64_t)gridDim.x * per) {
+    const float* p = in + row * group * A.Dk + d;
+    float s[V], x[V];
+    ldv<V>(p, s);
+#pragma unroll 4
+    for (int j = 1; j < group; ++j) {
+      ldv<V>(p + j * A.Dk, x);
+#pragma unroll
+      for (int i = 0; i < V; ++i) s[i] += x[i];
+    }
+    T* q = out + row * A.Dk + d;
+#pragma unroll
+    for (int i = 0; i < V; ++i) q[i] = from_f<T>(s[i]);
   }
 }
 
@@ -158,9 +166,11 @@ template <typename T> __global__ void __launch_bounds__(256) linattn_decay_kerne
 template <typename T> hipError_t reduce_t(const ReduceArgs& a) {
   const hipStream_t st = (hipStream_t)a.stream;
   if (a.dq32 && a.tokens > 0) {
-    const int64_t n = a.tokens * a.Hk * a.Dk;
-    const unsigned blocks = (unsigned)(n < 2048 * 256 ? (n + 255) / 256 : 2048);
-    hipLaunchKernelGGL(linattn_share_kernel<T>, dim3(blocks, 2), dim3(256), 0, st, a);
+    const int V = a.Dk % 4 == 0 ? 4 : 1;
+    const int64_t per = 256 / (a.Dk / V), n = (a.tokens * a.Hk + per - 1) / per;
+    const dim3 grid((unsigned)(n < 4096 ? n : 4096), 2);
+    if (V == 4) hipLaunchKernelGGL((linattn_share_kernel<T, 4>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((linattn_share_kernel<T, 1>), grid, dim3(256), 0, st, a);
   }
   if (a.da_piece) hipLaunchKernelGGL(linattn_decay_kernel<T>, dim3(a.H), dim3(256), 0, st, a);
   return hipGetLastError();

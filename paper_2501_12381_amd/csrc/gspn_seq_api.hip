@@ -251,12 +251,13 @@ extern "C" int gspn_linattn_fwd(const void* q, const void* k, const void* v, con
     la::StateArgs s{};
     s.g = p.g; s.x = in.k; s.y = in.v; s.x_shared = 1; s.Dx = p.Dk; s.Dy = p.Dv;
     s.a = log_decay; s.per_token = per_token; s.scale = scale; s.sx = p.Dv; s.sy = 1; s.stream = stream;
+    s.exact = final_state != nullptr;
     if (join_pieces(p, s, initial_state, start, (float*)(ws + l.gtot), stream) != hipSuccess) return GSPN_ERR_HIP;
   }
   la::FwdArgs f{};
   f.g = p.g; f.q = in.q; f.k = in.k; f.v = in.v; f.a = log_decay; f.per_token = per_token; f.scale = scale;
   f.s0 = initial_state; f.sf = final_state; f.start = start; f.o = o; f.stream = stream;
-  f.ovec = Dv % 4 == 0 && aligned(o, 4 * es);
+  f.ovec = Dv % 8 == 0 && aligned(o, 16);
   const hipError_t e = dtype == GSPN_F32 ? la::linattn_fwd_f32(f) : la::linattn_fwd_bf16(f);
   return e == hipSuccess ? GSPN_OK : GSPN_ERR_HIP;
 }
@@ -305,6 +306,7 @@ extern "C" int gspn_linattn_bwd(const void* dout, const void* q, const void* k, 
     la::StateArgs r{};
     r.g = p.g; r.x = in.q; r.y = rd; r.x_shared = 1; r.Dx = p.Dk; r.Dy = p.Dv; r.a = log_decay;
     r.per_token = per_token; r.scale = scale; r.reverse = 1; r.sx = p.Dv; r.sy = 1; r.stream = stream;
+    r.exact = dinitial_state != nullptr;
     if (join_pieces(p, r, dfinal_state, end, (float*)(ws + l.gtot_rev), stream) != hipSuccess) return GSPN_ERR_HIP;
   }
   s.mode = 1;
@@ -316,8 +318,8 @@ extern "C" int gspn_linattn_bwd(const void* dout, const void* q, const void* k, 
   b.g = p.g; b.q = in.q; b.k = in.k; b.v = in.v; b.dout = rd; b.a = log_decay; b.per_token = per_token;
   b.scale = scale; b.dsf = dfinal_state; b.ds0 = dinitial_state; b.end = end; b.chunks = ws + l.chunks;
   b.dq = dq; b.dk = dk; b.dv = dv; b.da = dlog_decay; b.stream = stream;
-  b.dkvec = Dk % 4 == 0 && (shared || (aligned(dq, 4 * es) && aligned(dk, 4 * es)));
-  b.dvvec = Dv % 4 == 0 && aligned(dv, 4 * es);
+  b.dkvec = Dk % 8 == 0 && (shared || (aligned(dq, 16) && aligned(dk, 16)));
+  b.dvvec = Dv % 8 == 0 && aligned(dv, 16);
   if (shared) {
     b.dq32 = (float*)(ws + l.dq32);
     b.dk32 = (float*)(ws + l.dk32);
