@@ -37,13 +37,6 @@ template <typename T, int KP, int VP> struct BwdLds {
   float x[NB];                 // <S, dM>
 };
 
-// sum over a wave's lanes, in every lane
-__device__ __forceinline__ float all_lanes(float v) {
-#pragma unroll
-  for (int k = 1; k < 64; k <<= 1) v += __shfl_xor(v, k);
-  return v;
-}
-
 // the dot of 16 registers of a result with the same lines of a row in LDS
 template <typename T> __device__ __forceinline__ float row_dot(const T* row, const f32x16& acc, int h) {
   float t = 0.f;
@@ -57,8 +50,9 @@ template <typename T> __device__ __forceinline__ float row_dot(const T* row, con
   return t;
 }
 
-template <typename T, int KP, int VP>
-__global__ void __launch_bounds__(2 * (KP + VP)) linattn_bwd_kernel(BwdArgs A) {
+// EXACT: the gradient of the initial states is returned
+template <typename T, int KP, int VP, bool EXACT>
+__global__ void __launch_bounds__(2 * (KP + VP), 2) linattn_bwd_kernel(BwdArgs A) {
   using E = Elem<T>;
   using Lds = BwdLds<T, KP, VP>;
   constexpr int C = E::kChunk, NC = C / 32;
@@ -69,7 +63,8 @@ __global__ void __launch_bounds__(2 * (KP + VP)) linattn_bwd_kernel(BwdArgs A) {
 
   const Geom& g = A.g;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, h = lane >> 5, l = pl(lane & 31);
-  const int head = blockIdx.x % g.H, pi = blockIdx.x / g.H;
+  int pi, head;
+  if (!find_work(g, pi, head)) return;
   const Piece pc = find_piece(g, pi);
   const int64_t slot = (int64_t)pi * g.H + head;
   if (pc.len < 0 || pc.seq >= g.N) {
@@ -130,7 +125,6 @@ __global__ void __launch_bounds__(2 * (KP + VP)) linattn_bwd_kernel(BwdArgs A) {
     f32x16 M[KP / 32];
     if (pc.last) state_read<KP>(M, A.dsf ? A.dsf + sidx : nullptr, g.Dk, g.Dv, g.Dv, 1, c0 + l, h);
     else state_read_regs<KP>(M, A.end + slot * (KP * VP), wave, lane);
-    const bool three = A.ds0 != nullptr;
     float da_sum = 0.f;  // wave 0, with one decay for the head
     for (int c = n - 1; c >= 0; --c) {
       const int t0 = c * C;
@@ -141,6 +135,7 @@ __global__ void __launch_bounds__(2 * (KP + VP)) linattn_bwd_kernel(BwdArgs A) {
       lds_barrier();
       if (c > 0) load(t0 - C);
       pair_table<T, KP>(s.dec, s.k, s.q, KS, A.scale, s.p, PS, wave, NA, lane);  // P[t][s]
+      __builtin_amdgcn_sched_barrier(0);
       // dv^T = dM^T k^T e^{G_C - G_s}
       f32x16 acc[NC];
 #pragma unroll
@@ -153,7 +148,8 @@ __global__ void __launch_bounds__(2 * (KP + VP)) linattn_bwd_kernel(BwdArgs A) {
       }
 #pragma unroll
       for (int ts = 0; ts < NC; ++ts) acc[ts] *= s.dec.kf[32 * ts + l];
-      state_add<T, KP>(M, s.q, KS, s.g, VS, c0, s.dec.qf, s.dec.tot, three, lane);
+      __builtin_amdgcn_sched_barrier(0);
+      state_add<T, KP, EXACT>(M, s.q, KS, s.g, VS, c0, s.dec.qf, s.dec.tot, lane);
       lds_barrier();
       // + do^T P
 #pragma unroll
@@ -180,23 +176,17 @@ __global__ void __launch_bounds__(2 * (KP + VP)) linattn_bwd_kernel(BwdArgs A) {
             w += s.w[b][lane];
           }
         }
-        const float own = w;
-#pragma unroll
-        for (int i = 1; i < 64; i <<= 1) {
-          const float fo = __shfl_down(f, i), wo = __shfl_up(w, i);
-          if (lane + i < 64) f += fo;
-          if (lane >= i) w += wo;
-        }
-        const float r = f + (w - own) + s.dec.tot * x;
+        const float fp = prefix_sum(f), wp = prefix_sum(w);
+        const float r = (lane_63(fp) - (fp - f)) + (wp - w) + s.dec.tot * x;
         if (lane < C && t0 + lane < pc.len) {
           if (A.per_token) da[(int64_t)(t0 + lane) * g.H] = from_f<T>(r);
           else da_sum += r;
         }
       }
     }
-    if (pc.first && A.ds0) state_write<KP>(M, A.ds0 + sidx, g.Dk, g.Dv, g.Dv, 1, c0 + l, h);
+    if (EXACT && pc.first) state_write<KP>(M, A.ds0 + sidx, g.Dk, g.Dv, g.Dv, 1, c0 + l, h);
     if (!A.per_token && wave == 0) {
-      da_sum = all_lanes(da_sum);
+      da_sum = lane_63(prefix_sum(da_sum));
       if (lane == 0) A.da_piece[slot] = da_sum;
     }
   } else {
@@ -218,6 +208,7 @@ __global__ void __launch_bounds__(2 * (KP + VP)) linattn_bwd_kernel(BwdArgs A) {
       lds_barrier();
       if (c > 0) load(t0 - C);
       pair_table<T, VP>(s.dec, s.v, s.g, VS, A.scale, s.z, PS, wb, NB, lane);  // Z[t][s]
+      __builtin_amdgcn_sched_barrier(0);
       // the terms through the states: dq^T = S do^T scale e^{G_t}, dk^T = dM v^T e^{G_C - G_s}
       f32x16 aq[NC], ak[NC];
 #pragma unroll
@@ -239,7 +230,7 @@ __global__ void __launch_bounds__(2 * (KP + VP)) linattn_bwd_kernel(BwdArgs A) {
         }
       }
       if (kAhead && c > 0) load_state(c - 1);
-      dot = all_lanes(dot);
+      dot = lane_63(prefix_sum(dot));
       if (lane == 0) s.x[wb] = dot;
       float w[NC];
 #pragma unroll
@@ -286,15 +277,18 @@ __global__ void __launch_bounds__(2 * (KP + VP)) linattn_bwd_kernel(BwdArgs A) {
   }
 }
 
-template <typename T, int KP, int VP> hipError_t linattn_bwd_launch(const BwdArgs& a) {
+template <typename T, int KP, int VP, bool EXACT> hipError_t linattn_bwd_start(const BwdArgs& a) {
   constexpr int bytes = sizeof(BwdLds<T, KP, VP>);
   static_assert(bytes <= 160 * 1024, "");
-  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&linattn_bwd_kernel<T, KP, VP>),
+  const auto kernel = &linattn_bwd_kernel<T, KP, VP, EXACT>;
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
                                            hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((linattn_bwd_kernel<T, KP, VP>), dim3((unsigned)((int64_t)a.g.pieces * a.g.H)),
-                     dim3(2 * (KP + VP)), bytes, (hipStream_t)a.stream, a);
+  hipLaunchKernelGGL(kernel, dim3(work_grid(a.g)), dim3(2 * (KP + VP)), bytes, (hipStream_t)a.stream, a);
   return hipGetLastError();
+}
+template <typename T, int KP, int VP> hipError_t linattn_bwd_launch(const BwdArgs& a) {
+  return a.ds0 ? linattn_bwd_start<T, KP, VP, true>(a) : linattn_bwd_start<T, KP, VP, false>(a);
 }
 
 template <typename T> hipError_t linattn_bwd_t(const BwdArgs& a) {

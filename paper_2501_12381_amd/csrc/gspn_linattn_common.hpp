@@ -53,8 +53,6 @@ template <> struct Elem<bf16> {
   // multiple apart for rows read along (8 lanes, 8 rows) and such that two
   // neighbouring slots of four rows differ, for reads down columns
   static constexpr int stride(int n) { return n + (n % 128 == 0 ? 24 : 8); }
-  // an fp32 value as a sum of bf16 ones: three carry all of its 24 bits, two 16
-  static constexpr int kParts = 3;
   struct Frag {
     bf16x8 v;
   };
@@ -66,11 +64,12 @@ template <> struct Elem<bf16> {
 #pragma unroll
     for (int j = 0; j < 8; ++j) x[j] = (float)f.v[j];
   }
-  // x = f[0] + f[1] (+ f[2]): upper halves cut off, the last part rounded
-  static __device__ __forceinline__ void split(const float* x, Frag* f, bool three) {
+  // x as a sum of N bf16 values: upper halves cut off, the last part rounded; three
+  // carry all of x's 24 bits, two 16
+  template <int N> static __device__ __forceinline__ void split(const float* x, Frag* f) {
     float r[8];
     cut(x, f[0], r);
-    if (three) {
+    if constexpr (N == 3) {
       float q[8];
       cut(r, f[1], q);
       set(f[2], q);
@@ -120,7 +119,6 @@ template <> struct Elem<float> {
   static constexpr int kChunk = 32;
   static constexpr int kVec = 4;
   static constexpr int stride(int n) { return n + 4; }
-  static constexpr int kParts = 1;
   struct Frag {
     float v[8];
   };
@@ -132,7 +130,7 @@ template <> struct Elem<float> {
 #pragma unroll
     for (int j = 0; j < 8; ++j) x[j] = f.v[j];
   }
-  static __device__ __forceinline__ void split(const float* x, Frag* f, bool) { set(f[0], x); }
+  template <int N> static __device__ __forceinline__ void split(const float* x, Frag* f) { set(f[0], x); }
   static __device__ __forceinline__ void mma(f32x16& c, const Frag& a, const Frag& b) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[j], b.v[j], c, 0, 0, 0);
@@ -192,6 +190,19 @@ __device__ __forceinline__ void lds_barrier() {
 // ---------------------------------------------------------------------------
 // pieces
 // ---------------------------------------------------------------------------
+// Workgroup -> (piece, head).  Workgroups go round the 8 dies in turn, each with an
+// L2 of its own; the value heads that share q and k stay on one die.
+__device__ __forceinline__ bool find_work(const Geom& g, int& piece, int& head) {
+  const int group = g.H / g.Hk, die = blockIdx.x & 7, i = blockIdx.x >> 3;
+  const int u = (i / group) * 8 + die;  // (piece, query/key head)
+  piece = u / g.Hk;
+  head = (u - piece * g.Hk) * group + i % group;
+  return piece < g.pieces;
+}
+inline unsigned work_grid(const Geom& g) {
+  return (unsigned)(((int64_t)g.pieces * g.Hk + 7) / 8 * 8 * (g.H / g.Hk));
+}
+
 // Batched sequences are cut at multiples of L tokens; piece i is piece i % P of
 // sequence i / P.  Packed ones are cut where the packed axis passes a multiple of
 // L: block b of the axis and sequence n meet in piece b + n, an index that no
@@ -324,15 +335,40 @@ __device__ __forceinline__ double load_decay(const T* __restrict__ a, int64_t st
   return g < -150.0 ? -150.0 : g;
 }
 
+// Moves within a wave without LDS: lanes without a source get 0.  ROWS: rows of
+// 16 lanes that take part.
+template <int CTRL, int ROWS = 0xf> __device__ __forceinline__ float moved(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, ROWS, 0xf, true));
+}
+template <int CTRL, int ROWS = 0xf> __device__ __forceinline__ double moved(double v) {
+  const long long x = __double_as_longlong(v);
+  const int lo = __builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, true);
+  const int hi = __builtin_amdgcn_update_dpp(0, (int)(x >> 32), CTRL, ROWS, 0xf, true);
+  return __longlong_as_double(((long long)hi << 32) | (unsigned)lo);
+}
+// sums of lanes 0..l: shifts by 1, 2, 4, 8 in a row, then the last lane of a row
+// to the next row, and of the lower half to the upper
+template <typename F> __device__ __forceinline__ F prefix_sum(F v) {
+  v += moved<0x111>(v);
+  v += moved<0x112>(v);
+  v += moved<0x114>(v);
+  v += moved<0x118>(v);
+  v += moved<0x142, 0xa>(v);
+  v += moved<0x143, 0xc>(v);
+  return v;
+}
+__device__ __forceinline__ float lane_63(float v) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63)); }
+__device__ __forceinline__ double lane_63(double v) {
+  const long long x = __double_as_longlong(v);
+  const int lo = __builtin_amdgcn_readlane((int)x, 63), hi = __builtin_amdgcn_readlane((int)(x >> 32), 63);
+  return __longlong_as_double(((long long)hi << 32) | (unsigned)lo);
+}
+
 // one wave; g: lane t's own term (0 past the chunk).  Returns G_C.
 template <typename T> __device__ __forceinline__ double chunk_decays(Decays<T>& d, double g, float scale, int lane) {
   constexpr int C = Elem<T>::kChunk;
-#pragma unroll
-  for (int k = 1; k < C; k <<= 1) {
-    const double o = __shfl_up(g, k);
-    if (lane >= k) g += o;
-  }
-  const double all = __shfl(g, C - 1);
+  g = prefix_sum(g);
+  const double all = lane_63(g);
   if (lane < C) {
     const float hi = (float)g;
     d.hi[lane] = hi;
@@ -412,33 +448,44 @@ __device__ __forceinline__ void pair_table(const Decays<T>& d, const T* a, const
 // in fp32 and given to the product in parts (Elem::split): two keep 16 bits, enough
 // for a state that only bf16 outputs are made of, three all 24, for one that is
 // returned (2 parts leave it 3e-6 off, one 2e-3).
-template <typename T, int XP>
+template <typename T, int XP, bool EXACT>
 __device__ __forceinline__ void state_add(f32x16* S, const T* x, int xstride, const T* y, int ystride, int ycol,
-                                          const float* f, float tot, bool three, int lane) {
-  constexpr int C = Elem<T>::kChunk, NP = Elem<T>::kParts;
+                                                const float* f, float tot, int lane) {
+  using E = Elem<T>;
+  using Frag = typename E::Frag;
+  constexpr int C = E::kChunk, NM = XP / 32, NP = sizeof(T) == 4 ? 1 : EXACT ? 3 : 2;
   const int h = lane >> 5;
+  // one step's operands are read while the one before is in the matrix unit; the
+  // fences keep the compiler from reading all steps' at once, which spills
+  Frag xf[NM], yf = col_frag(y, ystride, 0, ycol, lane);
 #pragma unroll
-  for (int m = 0; m < XP / 32; ++m) S[m] *= tot;
+  for (int m = 0; m < NM; ++m) xf[m] = col_frag(x, xstride, 0, 32 * m, lane);
+#pragma unroll
+  for (int m = 0; m < NM; ++m) S[m] *= tot;
 #pragma unroll
   for (int k0 = 0; k0 < C; k0 += 16) {
     float v[8];
-    Elem<T>::get(col_frag(y, ystride, k0, ycol, lane), v);
+    E::get(yf, v);
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] *= f[k0 + 8 * h + j];
-    typename Elem<T>::Frag p[NP];
-    Elem<T>::split(v, p, three);
+    Frag p[NP], xn[NM];
+    E::template split<NP>(v, p);
+    if (k0 + 16 < C) {
+      yf = col_frag(y, ystride, k0 + 16, ycol, lane);
 #pragma unroll
-    for (int m = 0; m < XP / 32; ++m) {
-      const auto xf = col_frag(x, xstride, k0, 32 * m, lane);
-      Elem<T>::mma(S[m], xf, p[0]);
-      if constexpr (NP > 1) {
-        Elem<T>::mma(S[m], xf, p[1]);
-        if (three) Elem<T>::mma(S[m], xf, p[2]);
-      }
+      for (int m = 0; m < NM; ++m) xn[m] = col_frag(x, xstride, k0 + 16, 32 * m, lane);
     }
+#pragma unroll
+    for (int i = 0; i < NP; ++i)
+#pragma unroll
+      for (int m = 0; m < NM; ++m) E::mma(S[m], xf[m], p[i]);
+    if (k0 + 16 < C) {
+#pragma unroll
+      for (int m = 0; m < NM; ++m) xf[m] = xn[m];
+    }
+    __builtin_amdgcn_sched_barrier(0);
   }
 }
-
 // S from / to (x, y)-strided fp32 memory (null: zero); y: this lane's line
 template <int XP>
 __device__ __forceinline__ void state_read(f32x16* S, const float* s, int Dx, int Dy, int sx, int sy, int y, int h) {

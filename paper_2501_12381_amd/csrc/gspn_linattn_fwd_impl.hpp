@@ -14,7 +14,9 @@
 namespace gspn {
 namespace la {
 
-template <typename T, int KP, int VP> __global__ void __launch_bounds__(2 * VP, 2) linattn_fwd_kernel(FwdArgs A) {
+// EXACT: the final state is returned
+template <typename T, int KP, int VP, bool EXACT>
+__global__ void __launch_bounds__(2 * VP, 2) linattn_fwd_kernel(FwdArgs A) {
   using E = Elem<T>;
   constexpr int C = E::kChunk, NT = 2 * VP, NW = VP / 32, NC = C / 32;
   constexpr int KS = E::stride(KP), VS = E::stride(VP), PS = E::stride(C);
@@ -23,7 +25,8 @@ template <typename T, int KP, int VP> __global__ void __launch_bounds__(2 * VP, 
 
   const Geom& g = A.g;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, h = lane >> 5, l = pl(lane & 31), c0 = 32 * wave;
-  const int head = blockIdx.x % g.H, pi = blockIdx.x / g.H;
+  int pi, head;
+  if (!find_work(g, pi, head)) return;
   const Piece pc = find_piece(g, pi);
   if (pc.len < 0) return;
   T* o = reinterpret_cast<T*>(A.o) + ((pc.batch * g.T + pc.t0) * g.H + head) * (int64_t)g.Dv;
@@ -37,7 +40,6 @@ template <typename T, int KP, int VP> __global__ void __launch_bounds__(2 * VP, 
   const int64_t sidx = ((int64_t)pc.seq * g.H + head) * g.Dk * g.Dv;
   if (pc.first) state_read<KP>(S, A.s0 ? A.s0 + sidx : nullptr, g.Dk, g.Dv, g.Dv, 1, c0 + l, h);
   else state_read_regs<KP>(S, A.start + ((int64_t)pi * g.H + head) * (KP * VP), wave, lane);
-  const bool three = A.sf != nullptr;
 
   const T* a = reinterpret_cast<const T*>(A.a) + head +
                (A.per_token ? (pc.batch * g.T + pc.t0) * (int64_t)g.H : (int64_t)0);
@@ -66,6 +68,7 @@ template <typename T, int KP, int VP> __global__ void __launch_bounds__(2 * VP, 
     if (t0 + C < pc.len) load(t0 + C);
 
     pair_table<T, KP>(dec, sk, sq, KS, A.scale, sp, PS, wave, NW, lane);  // P[t][s]
+    __builtin_amdgcn_sched_barrier(0);
     // o^T = S^T q^T e^G: lines of v along the registers, lane = t
     f32x16 acc[NC];
 #pragma unroll
@@ -78,7 +81,8 @@ template <typename T, int KP, int VP> __global__ void __launch_bounds__(2 * VP, 
     }
 #pragma unroll
     for (int tt = 0; tt < NC; ++tt) acc[tt] *= dec.qf[32 * tt + l];
-    state_add<T, KP>(S, sk, KS, sv, VS, c0, dec.kf, dec.tot, three, lane);
+    __builtin_amdgcn_sched_barrier(0);
+    state_add<T, KP, EXACT>(S, sk, KS, sv, VS, c0, dec.kf, dec.tot, lane);
     lds_barrier();
     // + v^T P^T
 #pragma unroll
@@ -93,18 +97,23 @@ template <typename T, int KP, int VP> __global__ void __launch_bounds__(2 * VP, 
     orow += C * ot;
     lds_barrier();
   }
-  if (pc.last && A.sf) state_write<KP>(S, A.sf + sidx, g.Dk, g.Dv, g.Dv, 1, c0 + l, h);
+  if (EXACT && pc.last) state_write<KP>(S, A.sf + sidx, g.Dk, g.Dv, g.Dv, 1, c0 + l, h);
+}
+
+template <typename T, int KP, int VP> hipError_t linattn_fwd_launch(const FwdArgs& a) {
+  const dim3 grid(work_grid(a.g)), block(2 * VP);
+  const hipStream_t st = (hipStream_t)a.stream;
+  if (a.sf) hipLaunchKernelGGL((linattn_fwd_kernel<T, KP, VP, true>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((linattn_fwd_kernel<T, KP, VP, false>), grid, block, 0, st, a);
+  return hipGetLastError();
 }
 
 template <typename T> hipError_t linattn_fwd_t(const FwdArgs& a) {
-  const dim3 grid((unsigned)((int64_t)a.g.pieces * a.g.H));
-  const hipStream_t st = (hipStream_t)a.stream;
   const bool kw = a.g.Dk > 64, vw = a.g.Dv > 64;
-  if (kw && vw) hipLaunchKernelGGL((linattn_fwd_kernel<T, 128, 128>), grid, dim3(256), 0, st, a);
-  else if (kw) hipLaunchKernelGGL((linattn_fwd_kernel<T, 128, 64>), grid, dim3(128), 0, st, a);
-  else if (vw) hipLaunchKernelGGL((linattn_fwd_kernel<T, 64, 128>), grid, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((linattn_fwd_kernel<T, 64, 64>), grid, dim3(128), 0, st, a);
-  return hipGetLastError();
+  if (kw && vw) return linattn_fwd_launch<T, 128, 128>(a);
+  if (kw) return linattn_fwd_launch<T, 128, 64>(a);
+  if (vw) return linattn_fwd_launch<T, 64, 128>(a);
+  return linattn_fwd_launch<T, 64, 64>(a);
 }
 
 }  // namespace la

@@ -13,7 +13,8 @@
 namespace gspn {
 namespace la {
 
-template <typename T, int XP, int YP> __global__ void __launch_bounds__(2 * YP, 2) linattn_state_kernel(StateArgs A) {
+template <typename T, int XP, int YP, bool EXACT>
+__global__ void __launch_bounds__(2 * YP, 2) linattn_state_kernel(StateArgs A) {
   constexpr int C = Elem<T>::kChunk, NT = 2 * YP;
   constexpr int XS = Elem<T>::stride(XP), YS = Elem<T>::stride(YP);
   __shared__ __align__(16) T sx[C * XS], sy[C * YS];
@@ -21,7 +22,8 @@ template <typename T, int XP, int YP> __global__ void __launch_bounds__(2 * YP, 
 
   const Geom& g = A.g;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, h = lane >> 5, l = pl(lane & 31);
-  const int head = blockIdx.x % g.H, pi = blockIdx.x / g.H;
+  int pi, head;
+  if (!find_work(g, pi, head)) return;
   const Piece pc = find_piece(g, pi);
   if (pc.len < 0 || pc.seq >= g.N) return;
   if (A.mode == 0 && (A.reverse ? pc.first : pc.last)) return;  // nobody reads its state
@@ -69,7 +71,7 @@ template <typename T, int XP, int YP> __global__ void __launch_bounds__(2 * YP, 
       for (int kk = 0; kk < XP / 16; ++kk)
         *reinterpret_cast<typename Elem<T>::Frag*>(out + kk * 512) = reg_frag<T>(S, kk);
     }
-    state_add<T, XP>(S, sx, XS, sy, YS, 32 * wave, f, dec.tot, A.exact, lane);
+    state_add<T, XP, EXACT>(S, sx, XS, sy, YS, 32 * wave, f, dec.tot, lane);
     lds_barrier();
   }
   if (A.mode == 0) {
@@ -78,15 +80,21 @@ template <typename T, int XP, int YP> __global__ void __launch_bounds__(2 * YP, 
   }
 }
 
-template <typename T> hipError_t linattn_state_t(const StateArgs& a) {
-  const dim3 grid((unsigned)((int64_t)a.g.pieces * a.g.H));
+template <typename T, int XP, int YP> hipError_t linattn_state_launch(const StateArgs& a) {
+  const dim3 grid(work_grid(a.g)), block(2 * YP);
   const hipStream_t st = (hipStream_t)a.stream;
-  const bool xw = a.Dx > 64, yw = a.Dy > 64;
-  if (xw && yw) hipLaunchKernelGGL((linattn_state_kernel<T, 128, 128>), grid, dim3(256), 0, st, a);
-  else if (xw) hipLaunchKernelGGL((linattn_state_kernel<T, 128, 64>), grid, dim3(128), 0, st, a);
-  else if (yw) hipLaunchKernelGGL((linattn_state_kernel<T, 64, 128>), grid, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((linattn_state_kernel<T, 64, 64>), grid, dim3(128), 0, st, a);
+  // fp32 products keep all bits anyway
+  if (a.exact && sizeof(T) == 2) hipLaunchKernelGGL((linattn_state_kernel<T, XP, YP, sizeof(T) == 2>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((linattn_state_kernel<T, XP, YP, false>), grid, block, 0, st, a);
   return hipGetLastError();
+}
+
+template <typename T> hipError_t linattn_state_t(const StateArgs& a) {
+  const bool xw = a.Dx > 64, yw = a.Dy > 64;
+  if (xw && yw) return linattn_state_launch<T, 128, 128>(a);
+  if (xw) return linattn_state_launch<T, 128, 64>(a);
+  if (yw) return linattn_state_launch<T, 64, 128>(a);
+  return linattn_state_launch<T, 64, 64>(a);
 }
 
 }  // namespace la
