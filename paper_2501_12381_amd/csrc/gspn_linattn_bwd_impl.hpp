@@ -32,9 +32,9 @@ template <typename T, int KP, int VP> struct BwdLds {
   static constexpr int KS = Elem<T>::stride(KP), VS = Elem<T>::stride(VP), PS = Elem<T>::stride(C);
   __align__(16) T q[C * KS], k[C * KS], v[C * VS], g[C * VS], p[C * PS], z[C * PS];
   __align__(16) T m[VP * KS];  // dM^T: [line of v][line of k]
-  Decays<T> dec;
-  float f[NB][C], w[NB][C];    // of each wave's lines of k: q.dq - k.dk + w, and w
-  float x[NB];                 // <S, dM>
+  Decays<T> dec[2];            // this chunk's and the next one's
+  float f[2][NB][C], w[2][NB][C];  // of each wave's lines of k: q.dq - k.dk + w, and w
+  float x[2][NB];              // <S, dM>
 };
 
 // the dot of 16 registers of a result with the same lines of a row in LDS
@@ -109,23 +109,53 @@ __global__ void __launch_bounds__(2 * (KP + VP), 2) linattn_bwd_kernel(BwdArgs A
     rk.load(left, A.k, -1);
     rv.load(left, A.v, -1);
     rg.load(left, A.dout, -1);
-    if (wave == 0 && lane < C) ra = load_decay(a + t * at, at, lane, left);
+  };
+  // the decays are the work of the last of the waves that own columns of v, which
+  // has none of the pairs: summed a chunk ahead, asked for two ahead
+  const bool decays = wave == NA - 1;
+  const auto ask = [&](int c) {
+    if (decays && lane < C && c >= 0) ra = load_decay(a + (int64_t)c * C * at, at, lane, pc.len - c * C);
   };
   const auto stage = [&] {
     rq.store(s.q);
     rk.store(s.k);
     rv.store(s.v);
     rg.store(s.g);
-    if (wave == 0) chunk_decays(s.dec, ra, A.scale, lane);
   };
-  if (n > 0) load(from);
+  if (n > 0) {
+    load(from);
+    ask(n - 1);
+    if (decays) chunk_decays(s.dec[(n - 1) & 1], ra, A.scale, lane);
+    ask(n - 2);
+  }
   // the two kinds of waves run loops of their own (the registers of the one are
   // then not kept through the other's code), with the same barriers
   if (va) {
     f32x16 M[KP / 32];
     if (pc.last) state_read<KP>(M, A.dsf ? A.dsf + sidx : nullptr, g.Dk, g.Dv, g.Dv, 1, c0 + l, h);
     else state_read_regs<KP>(M, A.end + slot * (KP * VP), wave, lane);
-    float da_sum = 0.f;  // wave 0, with one decay for the head
+    float da_sum = 0.f;  // with one decay for the head
+    // a chunk's da, from what the other waves left of it: suffix sums of f, prefix sums of w
+    const auto finish = [&](int c) {
+      const int e = c & 1;
+      float f = 0.f, w = 0.f, x = 0.f;
+#pragma unroll
+      for (int b = 0; b < NB; ++b) x += s.x[e][b];
+      if (lane < C) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          f += s.f[e][b][lane];
+          w += s.w[e][b][lane];
+        }
+      }
+      const float fp = prefix_sum(f), wp = prefix_sum(w);
+      const float r = (lane_63(fp) - (fp - f)) + (wp - w) + s.dec[e].tot * x;
+      const int t = c * C + lane;
+      if (lane < C && t < pc.len) {
+        if (A.per_token) da[(int64_t)t * g.H] = from_f<T>(r);
+        else da_sum += r;
+      }
+    };
     for (int c = n - 1; c >= 0; --c) {
       const int t0 = c * C;
       stage();
@@ -133,8 +163,14 @@ __global__ void __launch_bounds__(2 * (KP + VP), 2) linattn_bwd_kernel(BwdArgs A
       for (int kk = 0; kk < KP / 16; ++kk)
         *reinterpret_cast<typename E::Frag*>(s.m + (c0 + l) * KS + 16 * kk + 8 * h) = reg_frag<T>(M, kk);
       lds_barrier();
+      const Decays<T>& dec = s.dec[c & 1];
       if (c > 0) load(t0 - C);
-      pair_table<T, KP>(s.dec, s.k, s.q, KS, A.scale, s.p, PS, wave, NA, lane);  // P[t][s]
+      if (decays) {
+        if (c + 1 < n) finish(c + 1);  // whose decays' place the next chunk's take
+        if (c > 0) chunk_decays(s.dec[(c - 1) & 1], ra, A.scale, lane);
+        ask(c - 2);
+      }
+      pair_table<T, KP>(dec, s.k, s.q, KS, A.scale, s.p, PS, wave, NA, lane);  // P[t][s]
       __builtin_amdgcn_sched_barrier(0);
       // dv^T = dM^T k^T e^{G_C - G_s}
       f32x16 acc[NC];
@@ -147,9 +183,9 @@ __global__ void __launch_bounds__(2 * (KP + VP), 2) linattn_bwd_kernel(BwdArgs A
         for (int ts = 0; ts < NC; ++ts) E::mma(acc[ts], mf, row_frag(s.k, KS, 32 * ts + l, 16 * kk, h));
       }
 #pragma unroll
-      for (int ts = 0; ts < NC; ++ts) acc[ts] *= s.dec.kf[32 * ts + l];
+      for (int ts = 0; ts < NC; ++ts) acc[ts] *= dec.kf[32 * ts + l];
       __builtin_amdgcn_sched_barrier(0);
-      state_add<T, KP, EXACT>(M, s.q, KS, s.g, VS, c0, s.dec.qf, s.dec.tot, lane);
+      state_add<T, KP, EXACT>(M, s.q, KS, s.g, VS, c0, dec.qf, dec.tot, lane);
       lds_barrier();
       // + do^T P
 #pragma unroll
@@ -164,28 +200,10 @@ __global__ void __launch_bounds__(2 * (KP + VP), 2) linattn_bwd_kernel(BwdArgs A
         if (t < pc.len) put_lines(dv + t * vt + c0, acc[ts], g.Dv - c0, A.dvvec, h);
       }
       lds_barrier();
-      if (wave == 0) {
-        // suffix sums of f, prefix sums of w
-        float f = 0.f, w = 0.f, x = 0.f;
-#pragma unroll
-        for (int b = 0; b < NB; ++b) x += s.x[b];
-        if (lane < C) {
-#pragma unroll
-          for (int b = 0; b < NB; ++b) {
-            f += s.f[b][lane];
-            w += s.w[b][lane];
-          }
-        }
-        const float fp = prefix_sum(f), wp = prefix_sum(w);
-        const float r = (lane_63(fp) - (fp - f)) + (wp - w) + s.dec.tot * x;
-        if (lane < C && t0 + lane < pc.len) {
-          if (A.per_token) da[(int64_t)(t0 + lane) * g.H] = from_f<T>(r);
-          else da_sum += r;
-        }
-      }
     }
+    if (decays && n > 0) finish(0);
     if (EXACT && pc.first) state_write<KP>(M, A.ds0 + sidx, g.Dk, g.Dv, g.Dv, 1, c0 + l, h);
-    if (!A.per_token && wave == 0) {
+    if (!A.per_token && decays) {
       da_sum = lane_63(prefix_sum(da_sum));
       if (lane == 0) A.da_piece[slot] = da_sum;
     }
@@ -206,8 +224,9 @@ __global__ void __launch_bounds__(2 * (KP + VP), 2) linattn_bwd_kernel(BwdArgs A
       const int t0 = c * C;
       stage();
       lds_barrier();
+      const Decays<T>& dec = s.dec[c & 1];
       if (c > 0) load(t0 - C);
-      pair_table<T, VP>(s.dec, s.v, s.g, VS, A.scale, s.z, PS, wb, NB, lane);  // Z[t][s]
+      pair_table<T, VP>(dec, s.v, s.g, VS, A.scale, s.z, PS, wb, NB, lane);  // Z[t][s]
       __builtin_amdgcn_sched_barrier(0);
       // the terms through the states: dq^T = S do^T scale e^{G_t}, dk^T = dM v^T e^{G_C - G_s}
       f32x16 aq[NC], ak[NC];
@@ -231,13 +250,13 @@ __global__ void __launch_bounds__(2 * (KP + VP), 2) linattn_bwd_kernel(BwdArgs A
       }
       if (kAhead && c > 0) load_state(c - 1);
       dot = lane_63(prefix_sum(dot));
-      if (lane == 0) s.x[wb] = dot;
+      if (lane == 0) s.x[c & 1][wb] = dot;
       float w[NC];
 #pragma unroll
       for (int i = 0; i < NC; ++i) {
         const int t = 32 * i + l;
-        aq[i] *= s.dec.qf[t];
-        ak[i] *= s.dec.kf[t];
+        aq[i] *= dec.qf[t];
+        ak[i] *= dec.kf[t];
         w[i] = row_dot(s.k + t * KS + c0, ak[i], h);
       }
       lds_barrier();
@@ -258,8 +277,8 @@ __global__ void __launch_bounds__(2 * (KP + VP), 2) linattn_bwd_kernel(BwdArgs A
         f += __shfl_xor(f, 32);
         w[i] += __shfl_xor(w[i], 32);
         if (h == 0) {
-          s.f[wb][t] = f;
-          s.w[wb][t] = w[i];
+          s.f[c & 1][wb][t] = f;
+          s.w[c & 1][wb][t] = w[i];
         }
         if (t0 + t < pc.len) {
           const int64_t at = (t0 + t) * kt + c0;

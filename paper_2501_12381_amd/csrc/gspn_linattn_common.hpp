@@ -180,6 +180,13 @@ __device__ __forceinline__ float exp2_wide(double x) {
   return exp2_hw(hi) * __builtin_fmaf((float)(x - (double)hi), 0.6931472f, 1.f);
 }
 
+// Keeps what is computed from x where it is: the rare paths' conditions, hoisted out
+// of the loop over chunks, would take the scalar registers of the common ones.
+__device__ __forceinline__ int opaque(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
 // LDS barrier: global loads and stores stay in flight
 __device__ __forceinline__ void lds_barrier() {
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -283,18 +290,19 @@ template <typename T, int DP, int NT> struct Stage {
 #pragma unroll
       for (int i = 0; i < kPer; ++i) r[i] = *reinterpret_cast<const uint4*>(p + i * step);
     } else {
+      const int Dx = opaque(D), r0 = opaque(row);
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
-        const int at = row + i * kRows;
+        const int at = r0 + i * kRows;
         uint4 x = make_uint4(0, 0, 0, 0);
-        if (at < C && at < left && c < D) {
+        if (at < C && at < left && c < Dx) {
           const T* s = p + i * step;
           if (vec) {
             x = *reinterpret_cast<const uint4*>(s);
           } else {  // rows that are not whole 16-byte vectors
             T e[V];
 #pragma unroll
-            for (int j = 0; j < V; ++j) e[j] = c + j < D ? s[j] : (T)0.f;
+            for (int j = 0; j < V; ++j) e[j] = c + j < Dx ? s[j] : (T)0.f;
             x = __builtin_bit_cast(uint4, e);
           }
         }
@@ -314,18 +322,23 @@ template <typename T, int DP, int NT> struct Stage {
 // ---------------------------------------------------------------------------
 // a chunk's decays
 // ---------------------------------------------------------------------------
-// G_t in powers of two, summed in 64 bits.  In fp32 it is kept as two floats, so
-// that differences keep their digits behind a token whose decay is a reset (-inf,
-// taken as 2^-150: zero in fp32); in bf16 one float's are enough for P and Z, which
-// are rounded to bf16.
+// G_t in powers of two, summed in 64 bits.  For the pairs within a chunk,
+// e^{G_t - G_s} is a product of a factor of t and one of s, taken around the first
+// token of their half of the chunk (G_0', and e^{G_0' of the second half - of the first}
+// between the halves), as long as no factor passes 2^64.  Else (fast = 0, behind a
+// token that resets the state: -inf, taken as 2^-150, zero in fp32) it is formed
+// pair by pair from G, kept as two floats so that differences keep their digits.
 template <typename T> struct Decays {
   static constexpr int C = Elem<T>::kChunk;
-  float hi[C];         // G_t
-  float lo[C];
+  float ft[C];         // scale e^{G_t - G_0'}
+  float fs[C];         // e^{G_0' - G_s}
   float qf[C];         // scale e^{G_t}
   float kf[C];         // e^{G_C - G_t}
+  float hi[C], lo[C];  // G_t
   float tot;           // e^{G_C}
-  float pad[3];
+  float half;          // e^{G_0'' - G_0'}
+  int fast;
+  int pad;
 };
 
 template <typename T>
@@ -364,31 +377,54 @@ __device__ __forceinline__ double lane_63(double v) {
   return __longlong_as_double(((long long)hi << 32) | (unsigned)lo);
 }
 
+template <int LANE> __device__ __forceinline__ double from_lane(double v) {
+  const long long x = __double_as_longlong(v);
+  const int lo = __builtin_amdgcn_readlane((int)x, LANE), hi = __builtin_amdgcn_readlane((int)(x >> 32), LANE);
+  return __longlong_as_double(((long long)hi << 32) | (unsigned)lo);
+}
+
 // one wave; g: lane t's own term (0 past the chunk).  Returns G_C.
 template <typename T> __device__ __forceinline__ double chunk_decays(Decays<T>& d, double g, float scale, int lane) {
   constexpr int C = Elem<T>::kChunk;
   g = prefix_sum(g);
-  const double all = lane_63(g);
+  const double all = lane_63(g), g0 = from_lane<0>(g), g1 = from_lane<C / 2>(g);
+  const double own = g - (lane < C / 2 ? g0 : g1);
+  const bool small = own < 64.0 && own > -64.0;  // lanes past the chunk repeat its last token's G
+  const bool fast = __ballot(!small) == 0;
   if (lane < C) {
     const float hi = (float)g;
     d.hi[lane] = hi;
     d.lo[lane] = (float)(g - (double)hi);
+    const float e = exp2_wide(own);
+    d.ft[lane] = scale * e;
+    d.fs[lane] = exp2_wide(-own);
     d.qf[lane] = scale * exp2_wide(g);
     d.kf[lane] = exp2_wide(all - g);
   }
-  if (lane == 0) d.tot = exp2_wide(all);
+  if (lane == 0) {
+    d.tot = exp2_wide(all);
+    d.half = exp2_wide(g1 - g0);
+    d.fast = fast;
+  }
   return all;
 }
 
 // x[j] = raw[j] scale e^{G_t - G_{s+j}} for s + j <= t, 0 above
-template <typename T, int N>
+template <typename T, int N, bool DIAG>
 __device__ __forceinline__ void decayed(const Decays<T>& d, const float* raw, float scale, int t, int s, float* x) {
-  const float hi = d.hi[t], lo = sizeof(T) == 4 ? d.lo[t] : 0.f;
+  const int last = opaque(t - s);  // the compares, too, are cheaper than the registers that keep them
+  if (d.fast) {
+    const float ft = DIAG ? d.ft[t] : d.ft[t] * d.half;
 #pragma unroll
-  for (int j = 0; j < N; ++j) {
-    float e = hi - d.hi[s + j];
-    if constexpr (sizeof(T) == 4) e += lo - d.lo[s + j];
-    x[j] = s + j <= t ? raw[j] * (scale * exp2_hw(e)) : 0.f;
+    for (int j = 0; j < N; ++j) {
+      x[j] = raw[j] * ft * d.fs[s + j];
+      if (DIAG) x[j] = j <= last ? x[j] : 0.f;
+    }
+  } else {
+    const float hi = d.hi[t], lo = d.lo[t];
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      x[j] = j <= last ? raw[j] * (scale * exp2_hw((hi - d.hi[s + j]) + (lo - d.lo[s + j]))) : 0.f;
   }
 }
 
@@ -416,7 +452,8 @@ __device__ __forceinline__ void pair_table(const Decays<T>& d, const T* a, const
         float raw[8], x[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) raw[j] = acc[r + j];
-        decayed<T, 8>(d, raw, scale, t, s, x);
+        if (tile == 1) decayed<T, 8, false>(d, raw, scale, t, s, x);
+        else decayed<T, 8, true>(d, raw, scale, t, s, x);
         Elem<T>::store8(out + t * ostride + s, x);
       }
     } else {
@@ -433,7 +470,8 @@ __device__ __forceinline__ void pair_table(const Decays<T>& d, const T* a, const
           for (int j = 0; j < 8; ++j) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(fa.v[j], fb.v[j], acc, 0, 0, 0);
         }
         const float raw[4] = {acc[0], acc[1], acc[2], acc[3]};
-        decayed<T, 4>(d, raw, scale, t, s, x);
+        if (tile == 1) decayed<T, 4, false>(d, raw, scale, t, s, x);
+        else decayed<T, 4, true>(d, raw, scale, t, s, x);
       }
       *reinterpret_cast<float4*>(out + t * ostride + s) = make_float4(x[0], x[1], x[2], x[3]);
     }
@@ -524,6 +562,7 @@ template <int XP> __device__ __forceinline__ void state_write_regs(const f32x16*
 // the two runs of 8 lines that a result's registers are, to a row at p (line 0 of
 // the tile); left: lines of the tile that the row has; vec: whole runs, p aligned
 template <typename T> __device__ __forceinline__ void put_lines(T* p, const f32x16& acc, int left, int vec, int h) {
+  if (!vec) left = opaque(left);
 #pragma unroll
   for (int r = 0; r < 16; r += 8) {
     const int c = reg_line(r, h);

@@ -21,7 +21,7 @@ __global__ void __launch_bounds__(2 * VP, 2) linattn_fwd_kernel(FwdArgs A) {
   constexpr int C = E::kChunk, NT = 2 * VP, NW = VP / 32, NC = C / 32;
   constexpr int KS = E::stride(KP), VS = E::stride(VP), PS = E::stride(C);
   __shared__ __align__(16) T sq[C * KS], sk[C * KS], sv[C * VS], sp[C * PS];
-  __shared__ Decays<T> dec;
+  __shared__ Decays<T> decs[2];  // this chunk's and the next one's
 
   const Geom& g = A.g;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, h = lane >> 5, l = pl(lane & 31), c0 = 32 * wave;
@@ -55,17 +55,30 @@ __global__ void __launch_bounds__(2 * VP, 2) linattn_fwd_kernel(FwdArgs A) {
     rq.load(left, A.q, 1);
     rk.load(left, A.k, 1);
     rv.load(left, A.v, 1);
-    if (wave == 0 && lane < C) ra = load_decay(a + t * at, at, lane, left);
   };
-  if (pc.len > 0) load(0);
+  // the decays are the last wave's, which has the least of the pairs: summed a chunk
+  // ahead, asked for two ahead
+  const auto ask = [&](int t) {
+    if (wave == NW - 1 && lane < C) ra = load_decay(a + t * at, at, lane, pc.len - t);
+  };
+  if (pc.len > 0) {
+    load(0);
+    ask(0);
+    if (wave == NW - 1) chunk_decays(decs[0], ra, A.scale, lane);
+    ask(C);
+  }
   T* orow = o + l * ot + c0;
   for (int t0 = 0; t0 < pc.len; t0 += C) {
     rq.store(sq);
     rk.store(sk);
     rv.store(sv);
-    if (wave == 0) chunk_decays(dec, ra, A.scale, lane);
+    const Decays<T>& dec = decs[t0 / C & 1];
     lds_barrier();
-    if (t0 + C < pc.len) load(t0 + C);
+    if (t0 + C < pc.len) {
+      load(t0 + C);
+      if (wave == NW - 1) chunk_decays(decs[(t0 / C + 1) & 1], ra, A.scale, lane);
+      ask(t0 + 2 * C);
+    }
 
     pair_table<T, KP>(dec, sk, sq, KS, A.scale, sp, PS, wave, NW, lane);  // P[t][s]
     __builtin_amdgcn_sched_barrier(0);

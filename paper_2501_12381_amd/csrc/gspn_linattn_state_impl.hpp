@@ -18,7 +18,7 @@ __global__ void __launch_bounds__(2 * YP, 2) linattn_state_kernel(StateArgs A) {
   constexpr int C = Elem<T>::kChunk, NT = 2 * YP;
   constexpr int XS = Elem<T>::stride(XP), YS = Elem<T>::stride(YP);
   __shared__ __align__(16) T sx[C * XS], sy[C * YS];
-  __shared__ Decays<T> dec;
+  __shared__ Decays<T> decs[2];  // this chunk's and the next one's
 
   const Geom& g = A.g;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, h = lane >> 5, l = pl(lane & 31);
@@ -53,25 +53,35 @@ __global__ void __launch_bounds__(2 * YP, 2) linattn_state_kernel(StateArgs A) {
     const int left = pc.len - t;
     rx.load(left, A.x, dir);
     ry.load(left, A.y, dir);
-    if (wave == 0 && lane < C) ra = load_decay(a + t * at, at, lane, left);
+  };
+  const auto ask = [&](int t) {  // two chunks ahead
+    if (wave == 0 && lane < C && t >= 0) ra = load_decay(a + t * at, at, lane, pc.len - t);
   };
   T* chunks = reinterpret_cast<T*>(A.chunks);
-  const float* f = A.reverse ? dec.qf : dec.kf;
-  if (n > 0) load(from);
+  if (n > 0) {
+    load(from);
+    ask(from);
+    if (wave == 0) all += chunk_decays(decs[0], ra, A.scale, lane);
+    ask(from + dir * C);
+  }
   for (int i = 0; i < n; ++i) {
     const int c = A.reverse ? n - 1 - i : i;
     rx.store(sx);
     ry.store(sy);
-    if (wave == 0) all += chunk_decays(dec, ra, A.scale, lane);
+    const Decays<T>& dec = decs[i & 1];
     lds_barrier();
-    if (i + 1 < n) load((c + dir) * C);
+    if (i + 1 < n) {
+      load((c + dir) * C);
+      if (wave == 0) all += chunk_decays(decs[(i + 1) & 1], ra, A.scale, lane);
+      ask((c + 2 * dir) * C);
+    }
     if (A.mode == 1) {
       T* out = chunks + (((int64_t)pi * (g.L / C) + c) * g.H + head) * (XP * YP) + (wave * (XP / 16) * 64 + lane) * 8;
 #pragma unroll
       for (int kk = 0; kk < XP / 16; ++kk)
         *reinterpret_cast<typename Elem<T>::Frag*>(out + kk * 512) = reg_frag<T>(S, kk);
     }
-    state_add<T, XP, EXACT>(S, sx, XS, sy, YS, 32 * wave, f, dec.tot, lane);
+    state_add<T, XP, EXACT>(S, sx, XS, sy, YS, 32 * wave, A.reverse ? dec.qf : dec.kf, dec.tot, lane);
     lds_barrier();
   }
   if (A.mode == 0) {
