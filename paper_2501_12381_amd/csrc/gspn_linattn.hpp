@@ -66,8 +66,9 @@ struct StateArgs {
   void* chunks;            // pieces x (L / C) x H states
   void* stream;
 };
-hipError_t linattn_state_f32(const StateArgs& a);
-hipError_t linattn_state_bf16(const StateArgs& a);
+// b: a second walk of the same pieces in the same launch, or null
+hipError_t linattn_state_f32(const StateArgs& a, const StateArgs* b);
+hipError_t linattn_state_bf16(const StateArgs& a, const StateArgs* b);
 
 // Pieces' own states -> their start states (reverse: end states), in place.
 struct JoinArgs {
@@ -79,7 +80,7 @@ struct JoinArgs {
   int reverse;
   void* stream;
 };
-hipError_t linattn_join(const JoinArgs& a);
+hipError_t linattn_join(const JoinArgs& a, const JoinArgs* b);
 
 struct BwdArgs {
   Geom g;
@@ -130,7 +131,7 @@ struct StepArgs {
 hipError_t linattn_step(const StepArgs& a);
 
 // register-order size of a state, in elements (sides padded to 64 or 128)
-inline int pad_dim(int d) { return d <= 64 ? 64 : 128; }
+__host__ __device__ constexpr int pad_dim(int d) { return d <= 64 ? 64 : 128; }
 inline int chunk_len(int dtype) { return dtype == 0 ? 32 : 64; }
 constexpr int kMaxDim = 128;
 

@@ -64,7 +64,7 @@ __global__ void __launch_bounds__(2 * (KP + VP), 2) linattn_bwd_kernel(BwdArgs A
   const Geom& g = A.g;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, h = lane >> 5, l = pl(lane & 31);
   int pi, head;
-  if (!find_work(g, pi, head)) return;
+  if (!find_work(g, blockIdx.x, pi, head)) return;
   const Piece pc = find_piece(g, pi);
   const int64_t slot = (int64_t)pi * g.H + head;
   if (pc.len < 0 || pc.seq >= g.N) {

@@ -199,8 +199,8 @@ __device__ __forceinline__ void lds_barrier() {
 // ---------------------------------------------------------------------------
 // Workgroup -> (piece, head).  Workgroups go round the 8 dies in turn, each with an
 // L2 of its own; the value heads that share q and k stay on one die.
-__device__ __forceinline__ bool find_work(const Geom& g, int& piece, int& head) {
-  const int group = g.H / g.Hk, die = blockIdx.x & 7, i = blockIdx.x >> 3;
+__device__ __forceinline__ bool find_work(const Geom& g, int block, int& piece, int& head) {
+  const int group = g.H / g.Hk, die = block & 7, i = block >> 3;
   const int u = (i / group) * 8 + die;  // (piece, query/key head)
   piece = u / g.Hk;
   head = (u - piece * g.Hk) * group + i % group;

@@ -5,6 +5,6 @@
 namespace gspn {
 namespace la {
 hipError_t linattn_fwd_bf16(const FwdArgs& a) { return linattn_fwd_t<bf16>(a); }
-hipError_t linattn_state_bf16(const StateArgs& a) { return linattn_state_t<bf16>(a); }
+hipError_t linattn_state_bf16(const StateArgs& a, const StateArgs* b) { return linattn_state_t<bf16>(a, b); }
 }  // namespace la
 }  // namespace gspn

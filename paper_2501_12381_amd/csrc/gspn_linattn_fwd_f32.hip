@@ -5,6 +5,6 @@
 namespace gspn {
 namespace la {
 hipError_t linattn_fwd_f32(const FwdArgs& a) { return linattn_fwd_t<float>(a); }
-hipError_t linattn_state_f32(const StateArgs& a) { return linattn_state_t<float>(a); }
+hipError_t linattn_state_f32(const StateArgs& a, const StateArgs* b) { return linattn_state_t<float>(a, b); }
 }  // namespace la
 }  // namespace gspn

@@ -26,7 +26,7 @@ __global__ void __launch_bounds__(2 * VP, 2) linattn_fwd_kernel(FwdArgs A) {
   const Geom& g = A.g;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, h = lane >> 5, l = pl(lane & 31), c0 = 32 * wave;
   int pi, head;
-  if (!find_work(g, pi, head)) return;
+  if (!find_work(g, blockIdx.x, pi, head)) return;
   const Piece pc = find_piece(g, pi);
   if (pc.len < 0) return;
   T* o = reinterpret_cast<T*>(A.o) + ((pc.batch * g.T + pc.t0) * g.H + head) * (int64_t)g.Dv;

@@ -14,7 +14,9 @@ namespace gspn {
 namespace la {
 
 template <typename T, int XP, int YP, bool EXACT>
-__global__ void __launch_bounds__(2 * YP, 2) linattn_state_kernel(StateArgs A) {
+__global__ void __launch_bounds__(2 * YP, 2) linattn_state_kernel(StateArgs A0, StateArgs A1, int second) {
+  const bool two = (int)blockIdx.x >= second;  // the second of two walks
+  const StateArgs& A = two ? A1 : A0;
   constexpr int C = Elem<T>::kChunk, NT = 2 * YP;
   constexpr int XS = Elem<T>::stride(XP), YS = Elem<T>::stride(YP);
   __shared__ __align__(16) T sx[C * XS], sy[C * YS];
@@ -23,7 +25,7 @@ __global__ void __launch_bounds__(2 * YP, 2) linattn_state_kernel(StateArgs A) {
   const Geom& g = A.g;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, h = lane >> 5, l = pl(lane & 31);
   int pi, head;
-  if (!find_work(g, pi, head)) return;
+  if (!find_work(g, (int)blockIdx.x - (two ? second : 0), pi, head)) return;
   const Piece pc = find_piece(g, pi);
   if (pc.len < 0 || pc.seq >= g.N) return;
   if (A.mode == 0 && (A.reverse ? pc.first : pc.last)) return;  // nobody reads its state
@@ -90,21 +92,32 @@ __global__ void __launch_bounds__(2 * YP, 2) linattn_state_kernel(StateArgs A) {
   }
 }
 
-template <typename T, int XP, int YP> hipError_t linattn_state_launch(const StateArgs& a) {
-  const dim3 grid(work_grid(a.g)), block(2 * YP);
+template <typename T, int XP, int YP> hipError_t linattn_state_launch(const StateArgs& a, const StateArgs* b) {
+  const int n = (int)work_grid(a.g);
+  const dim3 grid((unsigned)(b ? 2 * n : n)), block(2 * YP);
   const hipStream_t st = (hipStream_t)a.stream;
   // fp32 products keep all bits anyway
-  if (a.exact && sizeof(T) == 2) hipLaunchKernelGGL((linattn_state_kernel<T, XP, YP, sizeof(T) == 2>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((linattn_state_kernel<T, XP, YP, false>), grid, block, 0, st, a);
+  if ((a.exact || (b && b->exact)) && sizeof(T) == 2)
+    hipLaunchKernelGGL((linattn_state_kernel<T, XP, YP, sizeof(T) == 2>), grid, block, 0, st, a, b ? *b : a, n);
+  else
+    hipLaunchKernelGGL((linattn_state_kernel<T, XP, YP, false>), grid, block, 0, st, a, b ? *b : a, n);
   return hipGetLastError();
 }
 
-template <typename T> hipError_t linattn_state_t(const StateArgs& a) {
+template <typename T> hipError_t linattn_state_one(const StateArgs& a, const StateArgs* b) {
   const bool xw = a.Dx > 64, yw = a.Dy > 64;
-  if (xw && yw) return linattn_state_launch<T, 128, 128>(a);
-  if (xw) return linattn_state_launch<T, 128, 64>(a);
-  if (yw) return linattn_state_launch<T, 64, 128>(a);
-  return linattn_state_launch<T, 64, 64>(a);
+  if (xw && yw) return linattn_state_launch<T, 128, 128>(a, b);
+  if (xw) return linattn_state_launch<T, 128, 64>(a, b);
+  if (yw) return linattn_state_launch<T, 64, 128>(a, b);
+  return linattn_state_launch<T, 64, 64>(a, b);
+}
+
+template <typename T> hipError_t linattn_state_t(const StateArgs& a, const StateArgs* b) {
+  if (b && (pad_dim(a.Dx) != pad_dim(b->Dx) || pad_dim(a.Dy) != pad_dim(b->Dy))) {  // other tiles: two launches
+    const hipError_t e = linattn_state_one<T>(a, nullptr);
+    return e == hipSuccess ? linattn_state_one<T>(*b, nullptr) : e;
+  }
+  return linattn_state_one<T>(a, b);
 }
 
 }  // namespace la

@@ -93,9 +93,17 @@ template <typename T> hipError_t step_t(const StepArgs& a) {
 // ---------------------------------------------------------------------------
 // join of a sequence's pieces: running = gtot running + local, in register order
 // ---------------------------------------------------------------------------
-__global__ void __launch_bounds__(256) linattn_join_kernel(JoinArgs A, int XP, int YP) {
+// A thread has four values of a state; kAhead pieces' are asked for together, as the
+// chain of a long sequence would otherwise wait for one load after another (100
+// pieces of 64 x 64: 29 us one by one, 12 us so).
+constexpr int kAhead = 8;
+
+__global__ void __launch_bounds__(256) linattn_join_kernel(JoinArgs A0, JoinArgs A1, int second) {
+  const bool two = (int)blockIdx.x >= second;
+  const JoinArgs& A = two ? A1 : A0;
   const Geom& g = A.g;
-  const int parts = XP * YP / 256, nh = blockIdx.x / parts, head = nh % g.H, n = nh / g.H;
+  const int block = (int)blockIdx.x - (two ? second : 0), XP = pad_dim(A.Dx), YP = pad_dim(A.Dy);
+  const int parts = XP * YP / 1024, nh = block / parts, head = nh % g.H, n = nh / g.H;
   int first, last;  // piece indexes
   if (g.cu) {
     const auto at = [&](int i) { return i == 0 ? 0 : max(0, min(g.T, (int)g.cu[i])); };
@@ -107,19 +115,43 @@ __global__ void __launch_bounds__(256) linattn_join_kernel(JoinArgs A, int XP, i
     last = first + g.P - 1;
   }
   if (first == last) return;
-  const int e = (blockIdx.x % parts) * 256 + threadIdx.x;  // register order: wave (y / 32), tile (x / 32), register, lane
-  const int lane = e & 63, r = (e >> 6) & 15, m = (e >> 10) % (XP / 32), w = (e >> 10) / (XP / 32);
-  const int x = 32 * m + reg_line(r, lane >> 5), y = 32 * w + pl(lane & 31);
+  const int e = ((block % parts) * 256 + threadIdx.x) * 4;  // wave (y / 32), tile (x / 32), register, lane
   const int64_t size = (int64_t)XP * YP;
-  float run = A.s0 && x < A.Dx && y < A.Dy
-                  ? A.s0[((int64_t)n * g.H + head) * A.Dx * A.Dy + x * A.sx + y * A.sy] : 0.f;
-  const int step = A.reverse ? -1 : 1, from = A.reverse ? last : first, to = A.reverse ? first : last;
-  float next = A.local[((int64_t)from * g.H + head) * size + e];
-  for (int i = from; i != to; i += step) {
-    run = __builtin_fmaf(A.gtot[(int64_t)i * g.H + head], run, next);
-    float* p = A.local + ((int64_t)(i + step) * g.H + head) * size + e;
-    if (i + step != to) next = *p;
-    *p = run;
+  float run[4] = {0.f, 0.f, 0.f, 0.f};
+  if (A.s0) {
+    const int r = (e >> 6) & 15, m = (e >> 10) % (XP / 32), w = (e >> 10) / (XP / 32);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int lane = (e & 63) + k, x = 32 * m + reg_line(r, lane >> 5), y = 32 * w + pl(lane & 31);
+      if (x < A.Dx && y < A.Dy) run[k] = A.s0[((int64_t)n * g.H + head) * A.Dx * A.Dy + x * A.sx + y * A.sy];
+    }
+  }
+  const int step = A.reverse ? -1 : 1, from = A.reverse ? last : first, count = last - first;
+  const int64_t pstep = step * (int64_t)g.H, vstep = pstep * size / 4;
+  const float* gt = A.gtot + (int64_t)from * g.H + head;
+  float4* p = reinterpret_cast<float4*>(A.local + ((int64_t)from * g.H + head) * size + e);
+  float4 ahead = *p;  // the round's first value: the round before writes its place
+  for (int i = 0; i < count; i += kAhead) {
+    float4 v[kAhead + 1];
+    float f[kAhead];
+    v[0] = ahead;
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      if (i + j < count) f[j] = gt[j * pstep];
+      if (i + j + 1 < count) v[j + 1] = p[(j + 1) * vstep];
+    }
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j)
+      if (i + j < count) {
+        run[0] = __builtin_fmaf(f[j], run[0], v[j].x);
+        run[1] = __builtin_fmaf(f[j], run[1], v[j].y);
+        run[2] = __builtin_fmaf(f[j], run[2], v[j].z);
+        run[3] = __builtin_fmaf(f[j], run[3], v[j].w);
+        p[(j + 1) * vstep] = make_float4(run[0], run[1], run[2], run[3]);
+      }
+    ahead = v[kAhead];
+    p += kAhead * vstep;
+    gt += kAhead * pstep;
   }
 }
 
@@ -180,10 +212,13 @@ template <typename T> hipError_t reduce_t(const ReduceArgs& a) {
 
 hipError_t linattn_step(const StepArgs& a) { return a.dtype == 0 ? step_t<float>(a) : step_t<bf16>(a); }
 
-hipError_t linattn_join(const JoinArgs& a) {
-  const int XP = pad_dim(a.Dx), YP = pad_dim(a.Dy);
-  hipLaunchKernelGGL(linattn_join_kernel, dim3((unsigned)((int64_t)(XP * YP / 256) * a.g.N * a.g.H)), dim3(256), 0,
-                     (hipStream_t)a.stream, a, XP, YP);
+hipError_t linattn_join(const JoinArgs& a, const JoinArgs* b) {
+  const auto blocks = [](const JoinArgs& j) {
+    return (int64_t)(pad_dim(j.Dx) * pad_dim(j.Dy) / 1024) * j.g.N * j.g.H;
+  };
+  const int64_t n = blocks(a), all = n + (b ? blocks(*b) : 0);
+  hipLaunchKernelGGL(linattn_join_kernel, dim3((unsigned)all), dim3(256), 0, (hipStream_t)a.stream, a, b ? *b : a,
+                     (int)n);
   return hipGetLastError();
 }
 

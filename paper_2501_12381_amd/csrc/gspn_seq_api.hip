@@ -53,32 +53,40 @@ struct Lin {
   int KP, VP, C;
 };
 
-// Sequences are cut where their heads alone would leave compute units idle.  A
-// piece is at least four chunks: its state is formed, joined and read again,
-// which costs about what three chunks' walk does.
-void make_geom(Lin* p, const int32_t* cu) {
-  const int64_t want = 512, T = p->T, C = p->C;
-  const int64_t units = p->packed ? 0 : p->N * p->H;
-  int64_t L;
-  const int64_t whole = (T + C - 1) / C * C;
+// Sequences are cut into pieces where their heads alone would leave compute units
+// idle.  `room` is how many workgroups of the call's main kernel the card holds at
+// once (256 compute units, by LDS and registers); a cut costs a walk of the
+// states and their join, about what half a main walk does.
+//   whole sequences: from 192 (sequence, head) pairs on; from 128 on with head sizes
+//   over 64 and less than 24 chunks; under 6 chunks.  Forward / backward in us, whole against
+//   cut: 256 pairs x 16 chunks of 128 values 69/198, 127/322; 128 x 16 60/155, 73/166;
+//   192 x 13 chunks of 64 46/96, 49/105; 120 x 32 88/203, 54/118; 64 x 8 39/72, 31/64.
+//   else as many pieces as there is room for, down to one chunk: a second round of
+//   workgroups costs more than longer pieces (64 pairs x 64 chunks of 128, forward with 512
+//   workgroups 94, with 1024 113; backward with 256 335, with 512 346).
+void make_geom(Lin* p, const int32_t* cu, bool bwd) {
+  const int64_t T = p->T, C = p->C, n = (T + C - 1) / C, pairs = p->N * p->H;
+  const bool wide = p->KP > 64 || p->VP > 64;
+  const int64_t room = bwd ? (wide ? 256 : 512) : (p->VP > 64 ? 512 : 1024);
+  int64_t L = n > 0 ? n : 1;  // chunks of a piece
   if (p->packed) {
-    L = (T * p->H + want - 1) / want;
-  } else if (units >= want / 2) {
-    L = whole;
-  } else {
-    const int64_t P = (want + units - 1) / units;
-    L = (T + P - 1) / P;
+    // pieces end at multiples of L tokens of the packed axis and at the sequences' ends
+    int64_t blocks = room / p->H - p->N;
+    if (blocks < room / (2 * p->H)) blocks = room / (2 * p->H);
+    if (blocks < 1) blocks = 1;
+    L = (n + blocks - 1) / blocks;
+  } else if (n >= 6 && pairs < 192 && !(wide && pairs >= 128 && n < 24) && pairs > 0) {
+    const int64_t P = room / pairs;
+    L = (n + P - 1) / P;
   }
-  L = (L + C - 1) / C * C;
-  if (L < 4 * C) L = 4 * C;
-  if (L > whole) L = whole > 0 ? whole : C;
+  if (L < 1) L = 1;
   la::Geom& g = p->g;
   g.cu = cu;
   g.N = (int)p->N;
   g.T = (int)T;
-  g.L = (int)L;
-  g.P = T > 0 ? (int)((T + L - 1) / L) : 1;
-  g.pieces = p->packed ? (int)(T / L + p->N + 1) : (int)(p->N * g.P);
+  g.L = (int)(L * C);
+  g.P = n > 0 ? (int)((n + L - 1) / L) : 1;
+  g.pieces = p->packed ? (int)(T / g.L + p->N + 1) : (int)(p->N * g.P);
   g.H = p->H;
   g.Hk = p->Hk;
   g.Dk = p->Dk;
@@ -86,7 +94,7 @@ void make_geom(Lin* p, const int32_t* cu) {
 }
 
 int check_lin(int64_t n_seq, int64_t B, int64_t T, int64_t H, int64_t Hk, int64_t Dk, int64_t Dv, int dtype,
-              uint32_t flags, bool packed, const int32_t* cu, Lin* p) {
+              uint32_t flags, bool packed, const int32_t* cu, bool bwd, Lin* p) {
   if (dtype != GSPN_F32 && dtype != GSPN_BF16) return GSPN_ERR_DTYPE;
   if (flags & ~(uint32_t)GSPN_LINATTN_DECAY_PER_TOKEN) return GSPN_ERR_UNSUPPORTED;
   if (n_seq < 0 || B < 0 || T < 0 || H < 1 || Hk < 1 || Dk < 1 || Dv < 1) return GSPN_ERR_SHAPE;
@@ -103,8 +111,8 @@ int check_lin(int64_t n_seq, int64_t B, int64_t T, int64_t H, int64_t Hk, int64_
   p->VP = la::pad_dim(p->Dv);
   p->C = la::chunk_len(dtype);
   if (n_seq == 0 && !packed) return GSPN_OK;
-  make_geom(p, cu);
-  // pieces and workgroups are counted in 32 bits (the join has 64 a head)
+  make_geom(p, cu, bwd);
+  // pieces and workgroups are counted in 32 bits (two joins have up to 32 a head)
   const int64_t pieces = packed ? T / p->g.L + n_seq + 1 : n_seq * p->g.P;
   if (pieces > 0x7fffffffLL / 64 / H) return GSPN_ERR_UNSUPPORTED;
   return GSPN_OK;
@@ -168,8 +176,8 @@ int lin_rows(const Lin& p, const void* ptr, int64_t heads, int D, const int64_t*
   return GSPN_OK;
 }
 
-hipError_t run_state(const Lin& p, const la::StateArgs& a) {
-  return p.dtype == GSPN_F32 ? la::linattn_state_f32(a) : la::linattn_state_bf16(a);
+hipError_t run_state(const Lin& p, const la::StateArgs& a, const la::StateArgs* b = nullptr) {
+  return p.dtype == GSPN_F32 ? la::linattn_state_f32(a, b) : la::linattn_state_bf16(a, b);
 }
 
 struct LinInputs {
@@ -192,15 +200,22 @@ int lin_inputs(const Lin& p, const void* q, const void* k, const void* v, const 
   return GSPN_OK;
 }
 
-// start states of the pieces (x along the registers)
-hipError_t join_pieces(const Lin& p, la::StateArgs s, const float* s0, float* local, float* gtot, void* stream) {
+// start states of the pieces, and with r (a reverse walk) their end states' gradients too
+hipError_t join_pieces(const Lin& p, la::StateArgs s, const float* s0, float* local, float* gtot,
+                       la::StateArgs* r = nullptr, const float* dsf = nullptr, float* rlocal = nullptr,
+                       float* rgtot = nullptr) {
+  if (p.N == 0) return hipSuccess;
   s.mode = 0;
   s.local = local;
   s.gtot = gtot;
-  hipError_t e = run_state(p, s);
-  if (e != hipSuccess || p.N == 0) return e;
-  la::JoinArgs j{p.g, local, gtot, s0, s.Dx, s.Dy, s.sx, s.sy, s.reverse, stream};
-  return la::linattn_join(j);
+  la::JoinArgs j{p.g, local, gtot, s0, s.Dx, s.Dy, s.sx, s.sy, s.reverse, s.stream}, k{};
+  if (r) {
+    r->local = rlocal;
+    r->gtot = rgtot;
+    k = la::JoinArgs{p.g, rlocal, rgtot, dsf, r->Dx, r->Dy, r->sx, r->sy, r->reverse, r->stream};
+  }
+  const hipError_t e = run_state(p, s, r);
+  return e == hipSuccess ? la::linattn_join(j, r ? &k : nullptr) : e;
 }
 
 }  // namespace
@@ -209,7 +224,7 @@ extern "C" size_t gspn_linattn_fwd_workspace_bytes(int64_t n_seq, int64_t B, int
                                                    int64_t Dk, int64_t Dv, int packed, gspn_dtype dtype,
                                                    uint32_t flags) {
   Lin p;
-  if (check_lin(n_seq, B, T, H, Hk, Dk, Dv, dtype, flags, packed, nullptr, &p) || nothing(p)) return 0;
+  if (check_lin(n_seq, B, T, H, Hk, Dk, Dv, dtype, flags, packed, nullptr, false, &p) || nothing(p)) return 0;
   return lin_layout(p, false).bytes;
 }
 
@@ -217,7 +232,7 @@ extern "C" size_t gspn_linattn_bwd_workspace_bytes(int64_t n_seq, int64_t B, int
                                                    int64_t Dk, int64_t Dv, int packed, gspn_dtype dtype,
                                                    uint32_t flags) {
   Lin p;
-  if (check_lin(n_seq, B, T, H, Hk, Dk, Dv, dtype, flags, packed, nullptr, &p) || nothing(p)) return 0;
+  if (check_lin(n_seq, B, T, H, Hk, Dk, Dv, dtype, flags, packed, nullptr, true, &p) || nothing(p)) return 0;
   return lin_layout(p, true).bytes;
 }
 
@@ -227,7 +242,7 @@ extern "C" int gspn_linattn_fwd(const void* q, const void* k, const void* v, con
                                 const int64_t* strides, gspn_dtype dtype, uint32_t flags, float scale,
                                 void* workspace, size_t workspace_bytes, void* stream) {
   Lin p;
-  int st = check_lin(n_seq, B, T, H, Hk, Dk, Dv, dtype, flags, cu_seqlens != nullptr, cu_seqlens, &p);
+  int st = check_lin(n_seq, B, T, H, Hk, Dk, Dv, dtype, flags, cu_seqlens != nullptr, cu_seqlens, false, &p);
   if (st || nothing(p)) return st;
   LinInputs in;
   if ((st = lin_inputs(p, q, k, v, log_decay, strides, &in))) return st;
@@ -252,7 +267,7 @@ extern "C" int gspn_linattn_fwd(const void* q, const void* k, const void* v, con
     s.g = p.g; s.x = in.k; s.y = in.v; s.x_shared = 1; s.Dx = p.Dk; s.Dy = p.Dv;
     s.a = log_decay; s.per_token = per_token; s.scale = scale; s.sx = p.Dv; s.sy = 1; s.stream = stream;
     s.exact = final_state != nullptr;
-    if (join_pieces(p, s, initial_state, start, (float*)(ws + l.gtot), stream) != hipSuccess) return GSPN_ERR_HIP;
+    if (join_pieces(p, s, initial_state, start, (float*)(ws + l.gtot)) != hipSuccess) return GSPN_ERR_HIP;
   }
   la::FwdArgs f{};
   f.g = p.g; f.q = in.q; f.k = in.k; f.v = in.v; f.a = log_decay; f.per_token = per_token; f.scale = scale;
@@ -269,7 +284,7 @@ extern "C" int gspn_linattn_bwd(const void* dout, const void* q, const void* k, 
                                 const int64_t* strides, gspn_dtype dtype, uint32_t flags, float scale,
                                 void* workspace, size_t workspace_bytes, void* stream) {
   Lin p;
-  int st = check_lin(n_seq, B, T, H, Hk, Dk, Dv, dtype, flags, cu_seqlens != nullptr, cu_seqlens, &p);
+  int st = check_lin(n_seq, B, T, H, Hk, Dk, Dv, dtype, flags, cu_seqlens != nullptr, cu_seqlens, true, &p);
   if (st || nothing(p)) return st;
   LinInputs in;
   if ((st = lin_inputs(p, q, k, v, log_decay, strides, &in))) return st;
@@ -302,12 +317,13 @@ extern "C" int gspn_linattn_bwd(const void* dout, const void* q, const void* k, 
   s.per_token = per_token; s.scale = scale; s.s0 = initial_state; s.sx = 1; s.sy = p.Dv; s.stream = stream;
   float *start = cut(p) ? (float*)(ws + l.start) : nullptr, *end = cut(p) ? (float*)(ws + l.end) : nullptr;
   if (cut(p)) {
-    if (join_pieces(p, s, initial_state, start, (float*)(ws + l.gtot), stream) != hipSuccess) return GSPN_ERR_HIP;
     la::StateArgs r{};
     r.g = p.g; r.x = in.q; r.y = rd; r.x_shared = 1; r.Dx = p.Dk; r.Dy = p.Dv; r.a = log_decay;
     r.per_token = per_token; r.scale = scale; r.reverse = 1; r.sx = p.Dv; r.sy = 1; r.stream = stream;
     r.exact = dinitial_state != nullptr;
-    if (join_pieces(p, r, dfinal_state, end, (float*)(ws + l.gtot_rev), stream) != hipSuccess) return GSPN_ERR_HIP;
+    if (join_pieces(p, s, initial_state, start, (float*)(ws + l.gtot), &r, dfinal_state, end,
+                    (float*)(ws + l.gtot_rev)) != hipSuccess)
+      return GSPN_ERR_HIP;
   }
   s.mode = 1;
   s.local = start;
@@ -340,7 +356,7 @@ extern "C" int gspn_linattn_step(const void* q, const void* k, const void* v, co
                                  int64_t Dk, int64_t Dv, const int64_t* strides, gspn_dtype dtype, uint32_t flags,
                                  float scale, void* stream) {
   Lin p;
-  int st = check_lin(B, B, 1, H, Hk, Dk, Dv, dtype, flags, false, nullptr, &p);
+  int st = check_lin(B, B, 1, H, Hk, Dk, Dv, dtype, flags, false, nullptr, false, &p);
   if (st) return st;
   if (n_slots < 0 || (!slots && n_slots < B)) return GSPN_ERR_SHAPE;
   int64_t states;
