@@ -289,13 +289,16 @@ int gspn_linattn_fwd(const void* q, const void* k, const void* v, const void* lo
 /* Gradients of <dout, o> + <dfinal_state, final_state>, fully overwritten:
  * dq, dk (B, T, Hk, Dk) summed over the value heads of each, dv, dlog_decay
  * shaped like log_decay, dinitial_state (NULL: not wanted).  dfinal_state may be
- * NULL (zero).  Nothing of the forward call is needed. */
+ * NULL (zero).  Nothing of the forward call is needed; forward_workspace, where it
+ * is not NULL, is the workspace of the forward call of the same problem (sizes,
+ * flags, cu_seqlens), of the size the query gives, unchanged since: the states it
+ * holds are then not formed again. */
 int gspn_linattn_bwd(const void* dout, const void* q, const void* k, const void* v, const void* log_decay,
                      const float* initial_state, const float* dfinal_state, const int32_t* cu_seqlens, void* dq,
                      void* dk, void* dv, void* dlog_decay, float* dinitial_state, int64_t n_seq, int64_t B,
                      int64_t T, int64_t H, int64_t Hk, int64_t Dk, int64_t Dv, const int64_t* strides,
-                     gspn_dtype dtype, uint32_t flags, float scale, void* workspace, size_t workspace_bytes,
-                     void* stream);
+                     gspn_dtype dtype, uint32_t flags, float scale, const void* forward_workspace,
+                     void* workspace, size_t workspace_bytes, void* stream);
 
 /* One token for each of B running sequences: state is updated in place, o
  * (B, H, Dv).  q, k (B, Hk, Dk), v (B, H, Dv); strides: batch row and head of

@@ -61,6 +61,10 @@ struct StateArgs {
   int mode;
   float* local;            // pieces x H register-order states
   float* gtot;             // pieces x H
+  // mode 1: start states that the forward call left, if `local` does not have them:
+  // its pieces are `ratio` to one of these, and its registers run along y
+  const float* fwd_start;
+  int ratio, fwd_pieces;   // fwd_pieces: of a batched sequence
   const float* s0;         // (N, H, Dk, Dv), or null
   int sx, sy;              // s0's strides along x and y
   void* chunks;            // pieces x (L / C) x H states

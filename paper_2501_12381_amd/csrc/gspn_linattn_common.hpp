@@ -552,6 +552,14 @@ template <int XP> __device__ __forceinline__ void state_read_regs(f32x16* S, con
 #pragma unroll
     for (int r = 0; r < 16; ++r) S[m][r] = s[((wave * (XP / 32) + m) * 16 + r) * 64 + lane];
 }
+// from the register order of the state's transpose (registers along y)
+template <int XP, int YP> __device__ __forceinline__ void state_read_turned(f32x16* S, const float* s, int y, int h) {
+  const int yr = y & 31, base = (y >> 5) * 16 + ((yr >> 4) << 3) + (yr & 7), half = ((yr >> 3) & 1) << 5;
+#pragma unroll
+  for (int m = 0; m < XP / 32; ++m)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) S[m][r] = s[(m * (YP / 32) * 16 + base) * 64 + half + pl(reg_line(r, h))];
+}
 template <int XP> __device__ __forceinline__ void state_write_regs(const f32x16* S, float* s, int wave, int lane) {
 #pragma unroll
   for (int m = 0; m < XP / 32; ++m)

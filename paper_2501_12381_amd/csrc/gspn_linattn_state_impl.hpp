@@ -38,6 +38,11 @@ __global__ void __launch_bounds__(2 * YP, 2) linattn_state_kernel(StateArgs A0, 
   } else if (pc.first) {
     state_read<XP>(S, A.s0 ? A.s0 + ((int64_t)pc.seq * g.H + head) * A.Dx * A.Dy : nullptr, A.Dx, A.Dy, A.sx, A.sy,
                    yc, h);
+  } else if (A.fwd_start) {
+    // the same place of the axis in the forward's pieces: block b of it is b * ratio there
+    const int block = pi - (g.cu ? pc.seq : pc.seq * g.P);
+    const int there = block * A.ratio + (g.cu ? pc.seq : pc.seq * A.fwd_pieces);
+    state_read_turned<XP, YP>(S, A.fwd_start + ((int64_t)there * g.H + head) * (XP * YP), yc, h);
   } else {
     state_read_regs<XP>(S, A.local + slot * (XP * YP), wave, lane);
   }

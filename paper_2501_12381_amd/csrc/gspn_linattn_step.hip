@@ -96,7 +96,7 @@ template <typename T> hipError_t step_t(const StepArgs& a) {
 // A thread has four values of a state; kAhead pieces' are asked for together, as the
 // chain of a long sequence would otherwise wait for one load after another (100
 // pieces of 64 x 64: 29 us one by one, 12 us so).
-constexpr int kAhead = 8;
+constexpr int kAhead = 16;
 
 __global__ void __launch_bounds__(256) linattn_join_kernel(JoinArgs A0, JoinArgs A1, int second) {
   const bool two = (int)blockIdx.x >= second;

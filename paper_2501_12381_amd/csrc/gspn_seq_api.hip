@@ -64,7 +64,9 @@ struct Lin {
 //   else as many pieces as there is room for, down to one chunk: a second round of
 //   workgroups costs more than longer pieces (64 pairs x 64 chunks of 128, forward with 512
 //   workgroups 94, with 1024 113; backward with 256 335, with 512 346).
-void make_geom(Lin* p, const int32_t* cu, bool bwd) {
+// A backward's piece is a whole number of the forward's pieces: it starts from the
+// states that the forward left.
+int64_t piece_chunks(const Lin* p, bool bwd) {
   const int64_t T = p->T, C = p->C, n = (T + C - 1) / C, pairs = p->N * p->H;
   const bool wide = p->KP > 64 || p->VP > 64;
   const int64_t room = bwd ? (wide ? 256 : 512) : (p->VP > 64 ? 512 : 1024);
@@ -80,13 +82,22 @@ void make_geom(Lin* p, const int32_t* cu, bool bwd) {
     L = (n + P - 1) / P;
   }
   if (L < 1) L = 1;
+  if (bwd) {
+    const int64_t f = piece_chunks(p, false);
+    if (f < n) L = (L + f - 1) / f * f;
+  }
+  return L;
+}
+
+void make_geom(Lin* p, const int32_t* cu, bool bwd) {
+  const int64_t n = (p->T + p->C - 1) / p->C, L = piece_chunks(p, bwd);
   la::Geom& g = p->g;
   g.cu = cu;
   g.N = (int)p->N;
-  g.T = (int)T;
-  g.L = (int)(L * C);
+  g.T = (int)p->T;
+  g.L = (int)(L * p->C);
   g.P = n > 0 ? (int)((n + L - 1) / L) : 1;
-  g.pieces = p->packed ? (int)(T / g.L + p->N + 1) : (int)(p->N * g.P);
+  g.pieces = p->packed ? (int)(p->T / g.L + p->N + 1) : (int)(p->N * g.P);
   g.H = p->H;
   g.Hk = p->Hk;
   g.Dk = p->Dk;
@@ -200,22 +211,20 @@ int lin_inputs(const Lin& p, const void* q, const void* k, const void* v, const 
   return GSPN_OK;
 }
 
-// start states of the pieces, and with r (a reverse walk) their end states' gradients too
-hipError_t join_pieces(const Lin& p, la::StateArgs s, const float* s0, float* local, float* gtot,
-                       la::StateArgs* r = nullptr, const float* dsf = nullptr, float* rlocal = nullptr,
-                       float* rgtot = nullptr) {
+la::JoinArgs join_args(const Lin& p, const la::StateArgs& s, const float* s0) {
+  return la::JoinArgs{p.g, s.local, s.gtot, s0, s.Dx, s.Dy, s.sx, s.sy, s.reverse, s.stream};
+}
+
+// start states of the pieces from walks of their own, and of r's (a reverse walk) too
+hipError_t join_pieces(const Lin& p, const la::StateArgs& s, const float* s0, const la::StateArgs* r = nullptr,
+                       const float* dsf = nullptr) {
   if (p.N == 0) return hipSuccess;
-  s.mode = 0;
-  s.local = local;
-  s.gtot = gtot;
-  la::JoinArgs j{p.g, local, gtot, s0, s.Dx, s.Dy, s.sx, s.sy, s.reverse, s.stream}, k{};
-  if (r) {
-    r->local = rlocal;
-    r->gtot = rgtot;
-    k = la::JoinArgs{p.g, rlocal, rgtot, dsf, r->Dx, r->Dy, r->sx, r->sy, r->reverse, r->stream};
-  }
   const hipError_t e = run_state(p, s, r);
-  return e == hipSuccess ? la::linattn_join(j, r ? &k : nullptr) : e;
+  if (e != hipSuccess) return e;
+  const la::JoinArgs j = join_args(p, s, s0);
+  if (!r) return la::linattn_join(j, nullptr);
+  const la::JoinArgs k = join_args(p, *r, dsf);
+  return la::linattn_join(j, &k);
 }
 
 }  // namespace
@@ -267,7 +276,8 @@ extern "C" int gspn_linattn_fwd(const void* q, const void* k, const void* v, con
     s.g = p.g; s.x = in.k; s.y = in.v; s.x_shared = 1; s.Dx = p.Dk; s.Dy = p.Dv;
     s.a = log_decay; s.per_token = per_token; s.scale = scale; s.sx = p.Dv; s.sy = 1; s.stream = stream;
     s.exact = final_state != nullptr;
-    if (join_pieces(p, s, initial_state, start, (float*)(ws + l.gtot)) != hipSuccess) return GSPN_ERR_HIP;
+    s.local = start; s.gtot = (float*)(ws + l.gtot);
+    if (join_pieces(p, s, initial_state) != hipSuccess) return GSPN_ERR_HIP;
   }
   la::FwdArgs f{};
   f.g = p.g; f.q = in.q; f.k = in.k; f.v = in.v; f.a = log_decay; f.per_token = per_token; f.scale = scale;
@@ -282,8 +292,9 @@ extern "C" int gspn_linattn_bwd(const void* dout, const void* q, const void* k, 
                                 void* dq, void* dk, void* dv, void* dlog_decay, float* dinitial_state, int64_t n_seq,
                                 int64_t B, int64_t T, int64_t H, int64_t Hk, int64_t Dk, int64_t Dv,
                                 const int64_t* strides, gspn_dtype dtype, uint32_t flags, float scale,
-                                void* workspace, size_t workspace_bytes, void* stream) {
-  Lin p;
+                                const void* forward_workspace, void* workspace, size_t workspace_bytes,
+                                void* stream) {
+  Lin p, pf;
   int st = check_lin(n_seq, B, T, H, Hk, Dk, Dv, dtype, flags, cu_seqlens != nullptr, cu_seqlens, true, &p);
   if (st || nothing(p)) return st;
   LinInputs in;
@@ -304,31 +315,52 @@ extern "C" int gspn_linattn_bwd(const void* dout, const void* q, const void* k, 
   const LinLayout l = lin_layout(p, true);
   if (!workspace || workspace_bytes < l.bytes) return GSPN_ERR_WORKSPACE;
   if (!aligned(workspace, 256)) return GSPN_ERR_ALIGN;
+  // the forward of the same problem, where it is cut too
+  if ((st = check_lin(n_seq, B, T, H, Hk, Dk, Dv, dtype, flags, cu_seqlens != nullptr, cu_seqlens, false, &pf)))
+    return st;
+  const LinLayout lf = lin_layout(pf, false);
+  if (!cut(p) || !cut(pf)) forward_workspace = nullptr;
+  if (!aligned(forward_workspace, 256)) return GSPN_ERR_ALIGN;
   const Span ins[] = {in.sq, in.sk, in.sv, in.sa, sd, span(initial_state, states, 4), span(dfinal_state, states, 4),
-                      span(cu_seqlens, n_seq + 1, 4)};
+                      span(cu_seqlens, n_seq + 1, 4), span(forward_workspace, (int64_t)lf.bytes, 1)};
   const Span outs[] = {span(dq, qk, es), span(dk, qk, es), span(dv, B * T * H * Dv, es),
                        span(dlog_decay, per_token ? B * T * H : H, es), span(dinitial_state, states, 4),
                        span(workspace, (int64_t)l.bytes, 1)};
   if ((st = check_spans(ins, outs))) return st;
   char* ws = (char*)workspace;
-  // states before each chunk (registers along v, lanes along k)
+  // registers along v, lanes along k
   la::StateArgs s{};
   s.g = p.g; s.x = in.v; s.y = in.k; s.y_shared = 1; s.Dx = p.Dv; s.Dy = p.Dk; s.a = log_decay;
   s.per_token = per_token; s.scale = scale; s.s0 = initial_state; s.sx = 1; s.sy = p.Dv; s.stream = stream;
-  float *start = cut(p) ? (float*)(ws + l.start) : nullptr, *end = cut(p) ? (float*)(ws + l.end) : nullptr;
+  la::StateArgs c = s;  // the states before each chunk
+  c.mode = 1;
+  c.chunks = ws + l.chunks;
+  float* end = nullptr;
   if (cut(p)) {
+    s.local = (float*)(ws + l.start);
+    s.gtot = (float*)(ws + l.gtot);
+    end = (float*)(ws + l.end);
     la::StateArgs r{};
     r.g = p.g; r.x = in.q; r.y = rd; r.x_shared = 1; r.Dx = p.Dk; r.Dy = p.Dv; r.a = log_decay;
     r.per_token = per_token; r.scale = scale; r.reverse = 1; r.sx = p.Dv; r.sy = 1; r.stream = stream;
     r.exact = dinitial_state != nullptr;
-    if (join_pieces(p, s, initial_state, start, (float*)(ws + l.gtot), &r, dfinal_state, end,
-                    (float*)(ws + l.gtot_rev)) != hipSuccess)
-      return GSPN_ERR_HIP;
+    r.local = end; r.gtot = (float*)(ws + l.gtot_rev);
+    if (forward_workspace) {
+      // the forward's start states: one walk fewer, and the other two in one launch
+      c.fwd_start = (const float*)((const char*)forward_workspace + lf.start);
+      c.ratio = p.g.L / pf.g.L;
+      c.fwd_pieces = pf.g.P;
+      const la::JoinArgs j = join_args(p, r, dfinal_state);
+      if (run_state(p, c, &r) != hipSuccess || (p.N > 0 && la::linattn_join(j, nullptr) != hipSuccess))
+        return GSPN_ERR_HIP;
+    } else {
+      c.local = s.local;
+      if (join_pieces(p, s, initial_state, &r, dfinal_state) != hipSuccess || run_state(p, c) != hipSuccess)
+        return GSPN_ERR_HIP;
+    }
+  } else if (run_state(p, c) != hipSuccess) {
+    return GSPN_ERR_HIP;
   }
-  s.mode = 1;
-  s.local = start;
-  s.chunks = ws + l.chunks;
-  if (run_state(p, s) != hipSuccess) return GSPN_ERR_HIP;
   const bool shared = p.H != p.Hk;
   la::BwdArgs b{};
   b.g = p.g; b.q = in.q; b.k = in.k; b.v = in.v; b.dout = rd; b.a = log_decay; b.per_token = per_token;

@@ -72,7 +72,7 @@ def load() -> ctypes.CDLL:
         fn.argtypes = [_i64] * 7 + [_i, _i, _u32]
         fn.restype = _sz
     lib.gspn_linattn_fwd.argtypes = [_p] * 8 + [_i64] * 7 + [_p, _i, _u32, _f, _p, _sz, _p]
-    lib.gspn_linattn_bwd.argtypes = [_p] * 13 + [_i64] * 7 + [_p, _i, _u32, _f, _p, _sz, _p]
+    lib.gspn_linattn_bwd.argtypes = [_p] * 13 + [_i64] * 7 + [_p, _i, _u32, _f, _p, _p, _sz, _p]
     lib.gspn_linattn_step.argtypes = [_p] * 7 + [_i64] * 6 + [_p, _i, _u32, _f, _p]
     for fn in (lib.gspn_group_norm_fwd_workspace_bytes, lib.gspn_group_norm_bwd_workspace_bytes):
         fn.argtypes = [_i64] * 4 + [_i]
@@ -138,11 +138,11 @@ def gspn_linattn_fwd(q, k, v, log_decay, initial_state, cu_seqlens, o, final_sta
 
 
 def gspn_linattn_bwd(dout, q, k, v, log_decay, initial_state, dfinal_state, cu_seqlens, dq, dk, dv, dlog_decay,
-                     dinitial_state, n_seq, B, T, H, Hk, Dk, Dv, strides, dtype, flags, scale, workspace,
-                     workspace_bytes, stream) -> int:
+                     dinitial_state, n_seq, B, T, H, Hk, Dk, Dv, strides, dtype, flags, scale, forward_workspace,
+                     workspace, workspace_bytes, stream) -> int:
     return int(load().gspn_linattn_bwd(dout, q, k, v, log_decay, initial_state, dfinal_state, cu_seqlens, dq, dk,
                                        dv, dlog_decay, dinitial_state, n_seq, B, T, H, Hk, Dk, Dv, strides, dtype,
-                                       flags, scale, workspace, workspace_bytes, stream))
+                                       flags, scale, forward_workspace, workspace, workspace_bytes, stream))
 
 
 def gspn_linattn_step(q, k, v, log_decay, state, slots, o, n_slots, B, H, Hk, Dk, Dv, strides, dtype, flags, scale,

@@ -123,14 +123,15 @@ class _Lin:
         return torch.empty(need, dtype=torch.uint8, device=self.dev) if need else None
 
 
-def gspn_linattn_fwd(q, k, v, log_decay, *, scale=None, initial_state=None, return_state: bool = False,
-                     cu_seqlens=None, workspace=None):
-    """(o, final state or None): S_t = exp(a_t) S_{t-1} + k_t v_t^T, o_t = scale q_t S_t.
+def gspn_linattn_workspace(q, k, v, log_decay, *, cu_seqlens=None) -> torch.Tensor:
+    """A workspace for the forward call, for programs that hand the states it keeps
+    there on to the backward (`forward_workspace`)."""
+    c = _Lin(q, k, v, log_decay, None, None, cu_seqlens)
+    ws = c.workspace(_lin_fwd_bytes, None)
+    return torch.empty(0, dtype=torch.uint8, device=c.dev) if ws is None else ws
 
-    q, k: (B, T, Hk, Dk); v: (B, T, H, Dv), H a multiple of Hk; log_decay: (H,) or
-    (B, T, H); scale: Dk ** -0.5 unless given.  States are float32 (n, H, Dk, Dv).
-    cu_seqlens (int32, n + 1 positions, on the GPU): n sequences packed into a
-    batch of one; else n = B."""
+
+def _linattn_fwd(q, k, v, log_decay, scale, initial_state, return_state, cu_seqlens, workspace):
     c = _Lin(q, k, v, log_decay, scale, initial_state, cu_seqlens)
     n, B, T, H, Hk, Dk, Dv = c.sizes
     o = torch.empty((B, T, H, Dv), dtype=q.dtype, device=c.dev)
@@ -139,12 +140,26 @@ def gspn_linattn_fwd(q, k, v, log_decay, *, scale=None, initial_state=None, retu
     _call(L.load().gspn_linattn_fwd, "gspn_linattn_fwd", c.dev, c.q.data_ptr(), c.k.data_ptr(), c.v.data_ptr(),
           c.a.data_ptr(), _ptr(c.s0), _ptr(c.cu), o.data_ptr(), _ptr(sf), *c.sizes, c.strides, c.dt, c.flags,
           c.scale, _ptr(ws), 0 if ws is None else ws.numel())
-    return o, sf
+    return o, sf, ws
+
+
+def gspn_linattn_fwd(q, k, v, log_decay, *, scale=None, initial_state=None, return_state: bool = False,
+                     cu_seqlens=None, workspace=None):
+    """(o, final state or None): S_t = exp(a_t) S_{t-1} + k_t v_t^T, o_t = scale q_t S_t.
+
+    q, k: (B, T, Hk, Dk); v: (B, T, H, Dv), H a multiple of Hk; log_decay: (H,) or
+    (B, T, H); scale: Dk ** -0.5 unless given.  States are float32 (n, H, Dk, Dv).
+    cu_seqlens (int32, n + 1 positions, on the GPU): n sequences packed into a
+    batch of one; else n = B."""
+    return _linattn_fwd(q, k, v, log_decay, scale, initial_state, return_state, cu_seqlens, workspace)[:2]
 
 
 def gspn_linattn_bwd(do, q, k, v, log_decay, *, scale=None, initial_state=None, dfinal_state=None, cu_seqlens=None,
-                     workspace=None):
-    """Gradients (dq, dk, dv, dlog_decay, dinitial_state or None) of <do, o> + <dfinal_state, final state>."""
+                     forward_workspace=None, workspace=None):
+    """Gradients (dq, dk, dv, dlog_decay, dinitial_state or None) of <do, o> + <dfinal_state, final state>.
+
+    forward_workspace: the workspace that the forward call on the same inputs was
+    given (gspn_linattn_workspace), unchanged since: its states are used again."""
     c = _Lin(q, k, v, log_decay, scale, initial_state, cu_seqlens)
     n, B, T, H, Hk, Dk, Dv = c.sizes
     _check_tensor("do", do, (B, T, H, Dv), q.dtype, c.dev, _LIN)
@@ -152,6 +167,11 @@ def gspn_linattn_bwd(do, q, k, v, log_decay, *, scale=None, initial_state=None, 
     if dfinal_state is not None:
         _check_tensor("dfinal_state", dfinal_state, (n, H, Dk, Dv), torch.float32, c.dev, _LIN)
         dfinal_state = dfinal_state.contiguous()
+    if forward_workspace is not None:
+        need = _lin_fwd_bytes(*c.sizes, int(c.packed), c.dt, c.flags)
+        if forward_workspace.numel() < need:
+            raise ValueError(f"the forward's workspace holds {forward_workspace.numel()} bytes, not {need}")
+        forward_workspace = c.workspace(_lin_fwd_bytes, forward_workspace) if need else None
     new = lambda t: torch.empty(t.shape, dtype=t.dtype, device=c.dev)  # noqa: E731
     dq, dk, dv = new(q), new(k), new(v)
     da = new(log_decay) if n else torch.zeros(log_decay.shape, dtype=q.dtype, device=c.dev)
@@ -159,8 +179,8 @@ def gspn_linattn_bwd(do, q, k, v, log_decay, *, scale=None, initial_state=None, 
     ws = c.workspace(_lin_bwd_bytes, workspace)
     _call(L.load().gspn_linattn_bwd, "gspn_linattn_bwd", c.dev, do.data_ptr(), c.q.data_ptr(), c.k.data_ptr(),
           c.v.data_ptr(), c.a.data_ptr(), _ptr(c.s0), _ptr(dfinal_state), _ptr(c.cu), dq.data_ptr(), dk.data_ptr(),
-          dv.data_ptr(), da.data_ptr(), _ptr(ds0), *c.sizes, c.strides, c.dt, c.flags, c.scale, _ptr(ws),
-          0 if ws is None else ws.numel())
+          dv.data_ptr(), da.data_ptr(), _ptr(ds0), *c.sizes, c.strides, c.dt, c.flags, c.scale,
+          _ptr(forward_workspace), _ptr(ws), 0 if ws is None else ws.numel())
     return dq, dk, dv, da, ds0
 
 
@@ -172,8 +192,8 @@ class GSPNLinAttn(torch.autograd.Function):
         ctx.save_for_backward(q, k, v, log_decay, initial_state, cu_seqlens)
         ctx.scale = scale
         ctx.set_materialize_grads(False)
-        o, sf = gspn_linattn_fwd(q, k, v, log_decay, scale=scale, initial_state=initial_state,
-                                 return_state=return_state, cu_seqlens=cu_seqlens)
+        # the workspace, if there is one, carries the states of the sequences' pieces to the backward
+        o, sf, ctx.ws = _linattn_fwd(q, k, v, log_decay, scale, initial_state, return_state, cu_seqlens, None)
         return (o, sf) if return_state else o
 
     @staticmethod
@@ -184,7 +204,7 @@ class GSPNLinAttn(torch.autograd.Function):
                 return (None,) * 8
             do = torch.zeros(v.shape, dtype=v.dtype, device=v.device)
         dq, dk, dv, da, ds0 = gspn_linattn_bwd(do, q, k, v, log_decay, scale=ctx.scale, initial_state=s0,
-                                               dfinal_state=dsf, cu_seqlens=cu)
+                                               dfinal_state=dsf, cu_seqlens=cu, forward_workspace=ctx.ws)
         return dq, dk, dv, da, ds0, None, None, None
 
 

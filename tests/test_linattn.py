@@ -282,6 +282,32 @@ def test_autograd(dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(1, 3000, 2, 1, 64, 64), (1, 2000, 2, 2, 128, 128), (3, 900, 4, 4, 128, 33),
+                                   (2, 1500, 3, 3, 24, 100), (1, 100, 2, 2, 16, 16)], ids=str)
+@pytest.mark.parametrize("packed", [False, True])
+def test_states_of_the_forward(shape, packed, dtype):
+    """The backward from the states that the forward left in its workspace."""
+    print(f"states of the forward {shape} packed {packed} {dtype}", flush=True)
+    B, T = shape[:2]
+    cu = [0, 1, T // 3, T // 3, T * B - 5] if packed else None
+    d = inputs(*((1, B * T) if packed else (B, T)), *shape[2:], dtype, True, 4 if packed else B, True, seed=T)
+    cut = torch.tensor(cu, dtype=torch.int32, device=DEV) if packed else None
+    args = (d["q"], d["k"], d["v"], d["a"])
+    ws = ops.gspn_linattn_workspace(*args, cu_seqlens=cut)
+    ops.gspn_linattn_fwd(*args, initial_state=d["s0"], cu_seqlens=cut, workspace=ws)
+    got = ops.gspn_linattn_bwd(d["do"], *args, initial_state=d["s0"], dfinal_state=d["dsf"], cu_seqlens=cut,
+                               forward_workspace=ws)
+    h = {k: np64(t) for k, t in d.items()}
+    ref = R.linattn(h["q"], h["k"], h["v"], h["a"], shape[4] ** -0.5, h["s0"], cu, h["do"], h["dsf"])
+    for name, x, y in zip(("dq", "dk", "dv", "da", "ds0"), got, ref[2:]):
+        close(x, y, F32 if name == "ds0" else dtype, name, 2 if name == "da" else 1)
+    if ws.numel():
+        with pytest.raises(ValueError):
+            ops.gspn_linattn_bwd(d["do"], *args, cu_seqlens=cut, forward_workspace=ws[:-256])
+
+
+@pytest.mark.gpu
 def test_repeats_and_streams():
     """The same bits every time, on another stream, and from a replayed graph."""
     d = inputs(1, 1500, 2, 1, 64, 64, BF16, True, 1, True)
