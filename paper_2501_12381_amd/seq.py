@@ -42,6 +42,9 @@ def _dtype(t: torch.Tensor, what: str) -> int:
 
 
 def _check_tensor(name, t, shape, dtype, dev, what) -> None:
+    # `dev` is a GPU's; the one test that all good tensors pass comes first
+    if isinstance(t, torch.Tensor) and t.dtype == dtype and t.shape == shape and t.device == dev:
+        return
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a tensor")
     if not t.is_cuda:
@@ -50,8 +53,7 @@ def _check_tensor(name, t, shape, dtype, dev, what) -> None:
         raise TypeError(f"{name} has dtype {t.dtype}, expected {dtype}")
     if t.device != dev:
         raise RuntimeError(f"{name} is on {t.device}, expected {dev}")
-    if t.shape != shape:
-        raise ValueError(f"{name} must be {tuple(shape)}, got {tuple(t.shape)}")
+    raise ValueError(f"{name} must be {tuple(shape)}, got {tuple(t.shape)}")
 
 
 def _ptr(t):
@@ -60,9 +62,11 @@ def _ptr(t):
 
 def _rows(t: torch.Tensor) -> torch.Tensor:
     """A tensor whose last axis is dense (other strides are passed on)."""
-    if t.stride(-1) == 1 and min(t.stride()) >= 0:
-        return t
-    return t.contiguous()
+    return t if t.is_contiguous() or t.stride(-1) == 1 else t.contiguous()
+
+
+def _needs_grad(*tensors) -> bool:
+    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
 
 
 # ---------------------------------------------------------------------------
@@ -112,7 +116,8 @@ class _Lin:
         q, k, v = _rows(q), _rows(k), _rows(v)
         self.q, self.k, self.v, self.a = q, k, v, log_decay.contiguous()
         self.s0, self.cu = initial_state, cu_seqlens
-        self.strides = _I64x9(*q.stride()[:3], *k.stride()[:3], *v.stride()[:3])
+        dense = q.is_contiguous() and k.is_contiguous() and v.is_contiguous()
+        self.strides = None if dense else _I64x9(*q.stride()[:3], *k.stride()[:3], *v.stride()[:3])
 
     def workspace(self, size, given):
         need = size(*self.sizes, int(self.packed), self.dt, self.flags)
@@ -131,16 +136,40 @@ def gspn_linattn_workspace(q, k, v, log_decay, *, cu_seqlens=None) -> torch.Tens
     return torch.empty(0, dtype=torch.uint8, device=c.dev) if ws is None else ws
 
 
-def _linattn_fwd(q, k, v, log_decay, scale, initial_state, return_state, cu_seqlens, workspace):
-    c = _Lin(q, k, v, log_decay, scale, initial_state, cu_seqlens)
+def _linattn_fwd(c: _Lin, return_state, workspace):
     n, B, T, H, Hk, Dk, Dv = c.sizes
-    o = torch.empty((B, T, H, Dv), dtype=q.dtype, device=c.dev)
+    o = torch.empty((B, T, H, Dv), dtype=c.q.dtype, device=c.dev)
     sf = torch.empty((n, H, Dk, Dv), dtype=torch.float32, device=c.dev) if return_state else None
     ws = c.workspace(_lin_fwd_bytes, workspace)
     _call(L.load().gspn_linattn_fwd, "gspn_linattn_fwd", c.dev, c.q.data_ptr(), c.k.data_ptr(), c.v.data_ptr(),
           c.a.data_ptr(), _ptr(c.s0), _ptr(c.cu), o.data_ptr(), _ptr(sf), *c.sizes, c.strides, c.dt, c.flags,
           c.scale, _ptr(ws), 0 if ws is None else ws.numel())
     return o, sf, ws
+
+
+def _linattn_bwd(c: _Lin, q, k, v, a, s0, cu, do, dsf, forward_workspace, workspace):
+    """c: the sizes of the call that q .. cu (dense on their last axis) belong to."""
+    _check_tensor("do", do, v.shape, q.dtype, c.dev, _LIN)
+    do = do.contiguous()
+    n, B, T, H, Hk, Dk, Dv = c.sizes
+    if dsf is not None:
+        _check_tensor("dfinal_state", dsf, (n, H, Dk, Dv), torch.float32, c.dev, _LIN)
+        dsf = dsf.contiguous()
+    if forward_workspace is not None:
+        need = _lin_fwd_bytes(*c.sizes, int(c.packed), c.dt, c.flags)
+        if forward_workspace.numel() < need:
+            raise ValueError(f"the forward's workspace holds {forward_workspace.numel()} bytes, not {need}")
+        forward_workspace = c.workspace(_lin_fwd_bytes, forward_workspace) if need else None
+    new = lambda t: torch.empty(t.shape, dtype=t.dtype, device=c.dev)  # noqa: E731
+    dq, dk, dv = new(q), new(k), new(v)
+    da = new(a) if n else torch.zeros(a.shape, dtype=q.dtype, device=c.dev)
+    ds0 = new(s0) if s0 is not None else None
+    ws = c.workspace(_lin_bwd_bytes, workspace)
+    _call(L.load().gspn_linattn_bwd, "gspn_linattn_bwd", c.dev, do.data_ptr(), q.data_ptr(), k.data_ptr(),
+          v.data_ptr(), a.data_ptr(), _ptr(s0), _ptr(dsf), _ptr(cu), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
+          da.data_ptr(), _ptr(ds0), *c.sizes, c.strides, c.dt, c.flags, c.scale, _ptr(forward_workspace), _ptr(ws),
+          0 if ws is None else ws.numel())
+    return dq, dk, dv, da, ds0
 
 
 def gspn_linattn_fwd(q, k, v, log_decay, *, scale=None, initial_state=None, return_state: bool = False,
@@ -151,7 +180,7 @@ def gspn_linattn_fwd(q, k, v, log_decay, *, scale=None, initial_state=None, retu
     (B, T, H); scale: Dk ** -0.5 unless given.  States are float32 (n, H, Dk, Dv).
     cu_seqlens (int32, n + 1 positions, on the GPU): n sequences packed into a
     batch of one; else n = B."""
-    return _linattn_fwd(q, k, v, log_decay, scale, initial_state, return_state, cu_seqlens, workspace)[:2]
+    return _linattn_fwd(_Lin(q, k, v, log_decay, scale, initial_state, cu_seqlens), return_state, workspace)[:2]
 
 
 def gspn_linattn_bwd(do, q, k, v, log_decay, *, scale=None, initial_state=None, dfinal_state=None, cu_seqlens=None,
@@ -161,27 +190,7 @@ def gspn_linattn_bwd(do, q, k, v, log_decay, *, scale=None, initial_state=None, 
     forward_workspace: the workspace that the forward call on the same inputs was
     given (gspn_linattn_workspace), unchanged since: its states are used again."""
     c = _Lin(q, k, v, log_decay, scale, initial_state, cu_seqlens)
-    n, B, T, H, Hk, Dk, Dv = c.sizes
-    _check_tensor("do", do, (B, T, H, Dv), q.dtype, c.dev, _LIN)
-    do = do.contiguous()
-    if dfinal_state is not None:
-        _check_tensor("dfinal_state", dfinal_state, (n, H, Dk, Dv), torch.float32, c.dev, _LIN)
-        dfinal_state = dfinal_state.contiguous()
-    if forward_workspace is not None:
-        need = _lin_fwd_bytes(*c.sizes, int(c.packed), c.dt, c.flags)
-        if forward_workspace.numel() < need:
-            raise ValueError(f"the forward's workspace holds {forward_workspace.numel()} bytes, not {need}")
-        forward_workspace = c.workspace(_lin_fwd_bytes, forward_workspace) if need else None
-    new = lambda t: torch.empty(t.shape, dtype=t.dtype, device=c.dev)  # noqa: E731
-    dq, dk, dv = new(q), new(k), new(v)
-    da = new(log_decay) if n else torch.zeros(log_decay.shape, dtype=q.dtype, device=c.dev)
-    ds0 = new(initial_state) if initial_state is not None else None
-    ws = c.workspace(_lin_bwd_bytes, workspace)
-    _call(L.load().gspn_linattn_bwd, "gspn_linattn_bwd", c.dev, do.data_ptr(), c.q.data_ptr(), c.k.data_ptr(),
-          c.v.data_ptr(), c.a.data_ptr(), _ptr(c.s0), _ptr(dfinal_state), _ptr(c.cu), dq.data_ptr(), dk.data_ptr(),
-          dv.data_ptr(), da.data_ptr(), _ptr(ds0), *c.sizes, c.strides, c.dt, c.flags, c.scale,
-          _ptr(forward_workspace), _ptr(ws), 0 if ws is None else ws.numel())
-    return dq, dk, dv, da, ds0
+    return _linattn_bwd(c, c.q, c.k, c.v, c.a, c.s0, c.cu, do, dfinal_state, forward_workspace, workspace)
 
 
 class GSPNLinAttn(torch.autograd.Function):
@@ -189,30 +198,33 @@ class GSPNLinAttn(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, q, k, v, log_decay, initial_state, scale, return_state, cu_seqlens):
-        ctx.save_for_backward(q, k, v, log_decay, initial_state, cu_seqlens)
-        ctx.scale = scale
-        ctx.set_materialize_grads(False)
+        c = _Lin(q, k, v, log_decay, scale, initial_state, cu_seqlens)
         # the workspace, if there is one, carries the states of the sequences' pieces to the backward
-        o, sf, ctx.ws = _linattn_fwd(q, k, v, log_decay, scale, initial_state, return_state, cu_seqlens, None)
+        o, sf, ctx.ws = _linattn_fwd(c, return_state, None)
+        ctx.save_for_backward(c.q, c.k, c.v, c.a, c.s0, c.cu)
+        c.q = c.k = c.v = c.a = c.s0 = c.cu = None
+        ctx.call = c
+        ctx.set_materialize_grads(False)
         return (o, sf) if return_state else o
 
     @staticmethod
     def backward(ctx, do, dsf=None):
-        q, k, v, log_decay, s0, cu = ctx.saved_tensors
+        if do is None and dsf is None:
+            return (None,) * 8
+        saved = ctx.saved_tensors
         if do is None:
-            if dsf is None:
-                return (None,) * 8
-            do = torch.zeros(v.shape, dtype=v.dtype, device=v.device)
-        dq, dk, dv, da, ds0 = gspn_linattn_bwd(do, q, k, v, log_decay, scale=ctx.scale, initial_state=s0,
-                                               dfinal_state=dsf, cu_seqlens=cu, forward_workspace=ctx.ws)
-        return dq, dk, dv, da, ds0, None, None, None
+            do = torch.zeros_like(saved[2], memory_format=torch.contiguous_format)
+        return (*_linattn_bwd(ctx.call, *saved, do, dsf, ctx.ws, None), None, None, None)
 
 
 def gspn_linattn(q, k, v, log_decay, *, scale=None, initial_state=None, return_state: bool = False,
                  cu_seqlens=None):
     """Differentiable linear attention with a decay for each head (arguments as in
     gspn_linattn_fwd): o, or (o, final state) with return_state."""
-    return GSPNLinAttn.apply(q, k, v, log_decay, initial_state, scale, return_state, cu_seqlens)
+    if _needs_grad(q, k, v, log_decay, initial_state):
+        return GSPNLinAttn.apply(q, k, v, log_decay, initial_state, scale, return_state, cu_seqlens)
+    o, sf, _ = _linattn_fwd(_Lin(q, k, v, log_decay, scale, initial_state, cu_seqlens), return_state, None)
+    return (o, sf) if return_state else o
 
 
 def gspn_linattn_step(q, k, v, log_decay, state, *, scale=None, slots=None, out=None) -> torch.Tensor:
@@ -254,7 +266,8 @@ def gspn_linattn_step(q, k, v, log_decay, state, *, scale=None, slots=None, out=
         _check_tensor("out", out, (B, H, Dv), q.dtype, dev, _LIN)
         if not out.is_contiguous():
             raise ValueError("out must be contiguous")
-    strides = _I64x6(*q.stride()[:2], *k.stride()[:2], *v.stride()[:2])
+    dense = q.is_contiguous() and k.is_contiguous() and v.is_contiguous()
+    strides = None if dense else _I64x6(*q.stride()[:2], *k.stride()[:2], *v.stride()[:2])
     _call(L.load().gspn_linattn_step, "gspn_linattn_step", dev, q.data_ptr(), k.data_ptr(), v.data_ptr(),
           log_decay.data_ptr(), state.data_ptr(), _ptr(slots), out.data_ptr(), n, B, H, Hk, Dk, Dv, strides, dt,
           L.GSPN_LINATTN_DECAY_PER_TOKEN if per_row else 0, Dk ** -0.5 if scale is None else float(scale))
@@ -348,4 +361,6 @@ class GSPNGroupNorm(torch.autograd.Function):
 
 def gspn_group_norm(x, groups: int, weight=None, bias=None, eps: float = 1e-5, act: str = "none") -> torch.Tensor:
     """Differentiable group norm with an activation on a channels-last x (B, ..., C)."""
-    return GSPNGroupNorm.apply(x, weight, bias, groups, eps, act)
+    if _needs_grad(x, weight, bias):
+        return GSPNGroupNorm.apply(x, weight, bias, groups, eps, act)
+    return gspn_group_norm_fwd(x, groups, weight, bias, eps=eps, act=act)[0]
