@@ -1,9 +1,10 @@
-"""Build libgspn.so (the HIP kernels and the C ABI) for gfx950 with hipcc.
+"""Build libgspn.so (the HIP kernels and the C ABI) for gfx950 with hipcc, and
+_binding.so (the torch binding of the sequence operators) with the host compiler.
 
     python -m paper_2501_12381_amd.build        # or __graft_entry__.build()
 
-Each source compiles to an object in parallel under _build/, then one link
-produces paper_2501_12381_amd/libgspn.so next to this file.
+Each source compiles to an object in parallel under _build/, then one link each
+produces the two libraries next to this file.
 """
 from __future__ import annotations
 
@@ -19,6 +20,7 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libgspn.so")
+BINDING = os.path.join(PKG, "_binding.so")
 ARCH = "gfx950"
 
 # packed fp32 ops are disabled: hipcc still vectorises plain float code, but
@@ -46,6 +48,27 @@ def sources() -> list[str]:
     names = sorted(f for f in os.listdir(CSRC) if f.endswith(".hip"))
     rank = lambda f: next((i for i, p in enumerate(SLOW_UNITS) if f.startswith(p)), len(SLOW_UNITS))
     return [os.path.join(CSRC, f) for f in sorted(names, key=rank)]
+
+
+def binding_commands() -> tuple[list[str], list[str]]:
+    """Compile and link commands of the torch binding (host code)."""
+    import sysconfig
+
+    import torch
+
+    root = os.path.dirname(torch.__file__)
+    rocm = os.environ.get("ROCM_PATH", "/opt/rocm")
+    inc = [f"-isystem{p}" for p in (os.path.join(root, "include"),
+                                    os.path.join(root, "include", "torch", "csrc", "api", "include"),
+                                    sysconfig.get_paths()["include"], os.path.join(rocm, "include"))]
+    obj = os.path.join(BUILD, "gspn_torch.o")
+    cxx = os.environ.get("CXX") or shutil.which("g++") or "c++"
+    compile_ = [cxx, "-O2", "-std=c++17", "-fPIC", "-D__HIP_PLATFORM_AMD__=1", "-DTORCH_EXTENSION_NAME=_binding",
+                f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", INCLUDE, *inc, "-MMD", "-MF",
+                obj[:-2] + ".d", "-c", os.path.join(CSRC, "gspn_torch.cpp"), "-o", obj]
+    link = [cxx, "-shared", "-o", BINDING + ".tmp", obj, "-L", PKG, "-l:libgspn.so", "-Wl,-rpath,$ORIGIN", "-L",
+            os.path.join(root, "lib"), "-ltorch", "-ltorch_cpu", "-ltorch_python", "-lc10", "-lc10_hip"]
+    return compile_, link
 
 
 def _run(cmd: list[str]) -> None:
@@ -85,6 +108,9 @@ def build(verbose: bool = False, jobs: int | None = None, incremental: bool = Fa
     objs = [os.path.join(BUILD, os.path.basename(s)[:-4] + ".o") for s in srcs]
     cmds = [[cc, *FLAGS, "-MMD", "-MF", o[:-2] + ".d", "-c", s, "-o", o] for s, o in zip(srcs, objs)
             if not (incremental and _up_to_date(o))]
+    compile_, link_binding = binding_commands()
+    if not (incremental and _up_to_date(compile_[-1])):
+        cmds.insert(0, compile_)
     if verbose:
         for c in cmds:
             print(" ".join(c), flush=True)
@@ -97,6 +123,10 @@ def build(verbose: bool = False, jobs: int | None = None, incremental: bool = Fa
         print(" ".join(link), flush=True)
     _run(link)
     os.replace(tmp, LIB)
+    if verbose:
+        print(" ".join(link_binding), flush=True)
+    _run(link_binding)
+    os.replace(BINDING + ".tmp", BINDING)
     return LIB
 
 

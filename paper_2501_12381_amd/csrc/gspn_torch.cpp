@@ -1,0 +1,412 @@
+// Torch binding of the sequence operators: argument checks, output and workspace
+// allocation and the autograd nodes, around the C ABI of libgspn.so.
+//
+// It is native because the host's time bounds these operators' small calls and
+// most training steps: an autograd node written in Python runs its backward on
+// the engine's thread, where taking the interpreter over costs more than the kernels
+// (a training step of a 14 x 14 stage: 185 us so, 60 us of them on the device).
+#include <c10/core/DeviceGuard.h>
+#include <c10/hip/HIPStream.h>
+#include <torch/extension.h>
+
+#include <optional>
+#include <stdexcept>
+#include <string>
+#include <tuple>
+
+#include "../../include/gspn.h"
+
+namespace {
+
+using at::Tensor;
+using std::optional;
+using torch::autograd::AutogradContext;
+using torch::autograd::variable_list;
+
+// a status of the library, raised in Python as lib.GSPNError
+struct Refused : std::runtime_error {
+  Refused(int s, const char* w) : std::runtime_error(std::string(w) + ": " + gspn_strerror(s)), status(s), where(w) {}
+  int status;
+  std::string where;
+};
+PyObject* g_error = nullptr;  // lib.GSPNError
+
+void ok(int status, const char* where) {
+  if (status != GSPN_OK) throw Refused(status, where);
+}
+
+constexpr const char* kLin = "linear attention";
+constexpr const char* kNorm = "group norm";
+
+gspn_dtype dtype_of(const Tensor& t, const char* what) {
+  if (t.scalar_type() == at::kFloat) return GSPN_F32;
+  TORCH_CHECK_TYPE(t.scalar_type() == at::kBFloat16, what, " supports float32 and bfloat16, got ", t.scalar_type());
+  return GSPN_BF16;
+}
+
+void check_gpu(const char* name, const Tensor& t, const char* what) {
+  TORCH_CHECK(t.is_cuda(), name, " is on ", t.device(), ": the ", what, " runs on the GPU only");
+}
+
+void check(const char* name, const Tensor& t, at::IntArrayRef shape, at::ScalarType dtype, at::Device dev,
+           const char* what) {
+  if (t.scalar_type() == dtype && t.device() == dev && t.sizes() == shape) return;
+  check_gpu(name, t, what);
+  TORCH_CHECK_TYPE(t.scalar_type() == dtype, name, " has dtype ", t.scalar_type(), ", expected ", dtype);
+  TORCH_CHECK(t.device() == dev, name, " is on ", t.device(), ", expected ", dev);
+  TORCH_CHECK_VALUE(t.sizes() == shape, name, " must be ", shape, ", got ", t.sizes());
+}
+
+void* ptr(const Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
+float* fptr(const Tensor& t) { return static_cast<float*>(ptr(t)); }
+Tensor given(const optional<Tensor>& t) { return t ? *t : Tensor(); }
+Tensor rows(const Tensor& t) { return t.is_contiguous() || t.stride(-1) == 1 ? t : t.contiguous(); }
+void* stream_of(const Tensor& t) { return c10::hip::getCurrentHIPStream(t.device().index()).stream(); }
+
+// a caller's workspace that is large enough, or a new one (undefined: none is needed)
+Tensor workspace(size_t need, const Tensor& have, const Tensor& like) {
+  if (have.defined() && have.numel() * have.element_size() >= (int64_t)need) {
+    if (need)
+      TORCH_CHECK_VALUE(have.device() == like.device() && have.is_contiguous() && have.scalar_type() == at::kByte,
+                        "workspace must be a contiguous uint8 tensor on ", like.device());
+    return have;
+  }
+  return need ? at::empty({(int64_t)need}, like.options().dtype(at::kByte)) : Tensor();
+}
+size_t bytes_of(const Tensor& t) { return t.defined() ? (size_t)t.numel() : 0; }
+
+// ---------------------------------------------------------------------------
+// linear attention
+// ---------------------------------------------------------------------------
+struct Lin {
+  Tensor q, k, v, a, s0, cu;  // dense on their last axis; s0, cu may be undefined
+  int64_t n, B, T, H, Hk, Dk, Dv;
+  gspn_dtype dt;
+  uint32_t flags;
+  float scale;
+  bool dense;
+  int64_t strides[9];
+
+  Lin(const Tensor& q_, const Tensor& k_, const Tensor& v_, const Tensor& a_, optional<double> scale_, Tensor s0_,
+      Tensor cu_) {
+    check_gpu("q", q_, kLin);
+    dt = dtype_of(q_, kLin);
+    TORCH_CHECK_VALUE(q_.dim() == 4 && v_.dim() == 4, "q must be (B, T, Hk, Dk) and v (B, T, H, Dv)");
+    const auto dev = q_.device();
+    const auto type = q_.scalar_type();
+    B = q_.size(0); T = q_.size(1); Hk = q_.size(2); Dk = q_.size(3);
+    H = v_.size(2); Dv = v_.size(3);
+    check("k", k_, q_.sizes(), type, dev, kLin);
+    check("v", v_, {B, T, H, Dv}, type, dev, kLin);
+    TORCH_CHECK_VALUE(Hk > 0 && H > 0 && H % Hk == 0, "v's ", H, " heads must be a multiple of q's and k's ", Hk);
+    const bool per_token = a_.dim() != 1;
+    if (per_token) check("log_decay", a_, {B, T, H}, type, dev, kLin);
+    else check("log_decay", a_, {H}, type, dev, kLin);
+    n = B;
+    if (cu_.defined()) {
+      TORCH_CHECK_VALUE(cu_.dim() == 1 && cu_.numel() >= 1,
+                        "cu_seqlens must be a tensor of the sequences' starts and the last one's end");
+      TORCH_CHECK_VALUE(B == 1, "packed sequences have one batch row, got ", B);
+      n = cu_.numel() - 1;
+      check("cu_seqlens", cu_, {n + 1}, at::kInt, dev, kLin);
+      cu = cu_.contiguous();
+    }
+    if (s0_.defined()) {
+      check("initial_state", s0_, {n, H, Dk, Dv}, at::kFloat, dev, kLin);
+      s0 = s0_.contiguous();
+    }
+    flags = per_token ? GSPN_LINATTN_DECAY_PER_TOKEN : 0;
+    scale = (float)(scale_ ? *scale_ : 1.0 / std::sqrt((double)Dk));
+    q = rows(q_); k = rows(k_); v = rows(v_); a = a_.contiguous();
+    dense = q.is_contiguous() && k.is_contiguous() && v.is_contiguous();
+    if (!dense)
+      for (int i = 0; i < 3; ++i) {
+        strides[i] = q.stride(i);
+        strides[3 + i] = k.stride(i);
+        strides[6 + i] = v.stride(i);
+      }
+  }
+  const int64_t* stride_ptr() const { return dense ? nullptr : strides; }
+  size_t fwd_bytes() const {
+    return gspn_linattn_fwd_workspace_bytes(n, B, T, H, Hk, Dk, Dv, cu.defined(), dt, flags);
+  }
+  size_t bwd_bytes() const {
+    return gspn_linattn_bwd_workspace_bytes(n, B, T, H, Hk, Dk, Dv, cu.defined(), dt, flags);
+  }
+};
+
+// o, final state (or undefined), workspace (or undefined)
+std::tuple<Tensor, Tensor, Tensor> lin_fwd(const Lin& c, bool return_state, const Tensor& have) {
+  const c10::DeviceGuard guard(c.q.device());
+  Tensor o = at::empty({c.B, c.T, c.H, c.Dv}, c.q.options()), sf;
+  if (return_state) sf = at::empty({c.n, c.H, c.Dk, c.Dv}, c.q.options().dtype(at::kFloat));
+  Tensor ws = workspace(c.fwd_bytes(), have, c.q);
+  ok(gspn_linattn_fwd(ptr(c.q), ptr(c.k), ptr(c.v), ptr(c.a), fptr(c.s0), static_cast<int32_t*>(ptr(c.cu)), ptr(o),
+                      fptr(sf), c.n, c.B, c.T, c.H, c.Hk, c.Dk, c.Dv, c.stride_ptr(), c.dt, c.flags, c.scale, ptr(ws),
+                      bytes_of(ws), stream_of(c.q)),
+     "gspn_linattn_fwd");
+  return {o, sf, ws};
+}
+
+// dq, dk, dv, dlog_decay, dinitial_state (or undefined)
+variable_list lin_bwd(const Lin& c, const Tensor& dout, Tensor dsf, Tensor fws, const Tensor& have) {
+  const c10::DeviceGuard guard(c.q.device());
+  check("do", dout, {c.B, c.T, c.H, c.Dv}, c.q.scalar_type(), c.q.device(), kLin);
+  const Tensor g = dout.contiguous();
+  if (dsf.defined()) {
+    check("dfinal_state", dsf, {c.n, c.H, c.Dk, c.Dv}, at::kFloat, c.q.device(), kLin);
+    dsf = dsf.contiguous();
+  }
+  if (fws.defined()) {
+    const size_t need = c.fwd_bytes();
+    TORCH_CHECK_VALUE(bytes_of(fws) >= need, "the forward's workspace holds ", fws.numel(), " bytes, not ", need);
+    fws = need ? workspace(need, fws, c.q) : Tensor();
+  }
+  const auto same = [&](const Tensor& t) { return at::empty(t.sizes(), t.options()); };
+  Tensor dq = same(c.q), dk = same(c.k), dv = same(c.v), ds0;
+  Tensor da = c.n ? same(c.a) : at::zeros(c.a.sizes(), c.a.options());
+  if (c.s0.defined()) ds0 = same(c.s0);
+  const Tensor ws = workspace(c.bwd_bytes(), have, c.q);
+  ok(gspn_linattn_bwd(ptr(g), ptr(c.q), ptr(c.k), ptr(c.v), ptr(c.a), fptr(c.s0), fptr(dsf),
+                      static_cast<int32_t*>(ptr(c.cu)), ptr(dq), ptr(dk), ptr(dv), ptr(da), fptr(ds0), c.n, c.B, c.T,
+                      c.H, c.Hk, c.Dk, c.Dv, c.stride_ptr(), c.dt, c.flags, c.scale, ptr(fws), ptr(ws), bytes_of(ws),
+                      stream_of(c.q)),
+     "gspn_linattn_bwd");
+  return {dq, dk, dv, da, ds0};
+}
+
+struct LinFn : torch::autograd::Function<LinFn> {
+  static variable_list forward(AutogradContext* ctx, const Tensor& q, const Tensor& k, const Tensor& v,
+                               const Tensor& a, const optional<Tensor>& s0, double scale, bool return_state,
+                               const optional<Tensor>& cu) {
+    const Lin c(q, k, v, a, scale, given(s0), given(cu));
+    auto [o, sf, ws] = lin_fwd(c, return_state, Tensor());
+    ctx->set_materialize_grads(false);
+    // the workspace, if there is one, carries the states of the sequences' pieces to the backward
+    ctx->save_for_backward({c.q, c.k, c.v, c.a, c.s0, c.cu});
+    ctx->saved_data["ws"] = ws.defined() ? at::IValue(ws) : at::IValue();
+    ctx->saved_data["scale"] = scale;
+    if (return_state) return {o, sf};
+    return {o};
+  }
+  static variable_list backward(AutogradContext* ctx, variable_list grads) {
+    Tensor dout = grads[0], dsf = grads.size() > 1 ? grads[1] : Tensor();
+    if (!dout.defined() && !dsf.defined()) return variable_list(8);
+    const auto s = ctx->get_saved_variables();
+    const Lin c(s[0], s[1], s[2], s[3], ctx->saved_data["scale"].toDouble(), s[4], s[5]);
+    if (!dout.defined()) dout = at::zeros(c.v.sizes(), c.v.options());
+    const at::IValue& ws = ctx->saved_data["ws"];
+    variable_list out = lin_bwd(c, dout, dsf, ws.isTensor() ? ws.toTensor() : Tensor(), Tensor());
+    out.resize(8);
+    return out;
+  }
+};
+
+variable_list linattn(const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& a, optional<double> scale,
+                      const optional<Tensor>& s0, bool return_state, const optional<Tensor>& cu) {
+  TORCH_CHECK_VALUE(q.dim() == 4, "q must be (B, T, Hk, Dk) and v (B, T, H, Dv)");
+  return LinFn::apply(q, k, v, a, s0, scale ? *scale : 1.0 / std::sqrt((double)std::max<int64_t>(q.size(3), 1)),
+                      return_state, cu);
+}
+
+Tensor linattn_step(const Tensor& q_, const Tensor& k_, const Tensor& v_, const Tensor& a_, const Tensor& state,
+                    optional<double> scale, const optional<Tensor>& slots_, const optional<Tensor>& out_) {
+  check_gpu("q", q_, kLin);
+  const gspn_dtype dt = dtype_of(q_, kLin);
+  TORCH_CHECK_VALUE(q_.dim() == 3 && v_.dim() == 3, "q must be (B, Hk, Dk) and v (B, H, Dv)");
+  const auto dev = q_.device();
+  const auto type = q_.scalar_type();
+  const int64_t B = q_.size(0), Hk = q_.size(1), Dk = q_.size(2), H = v_.size(1), Dv = v_.size(2);
+  check("k", k_, q_.sizes(), type, dev, kLin);
+  check("v", v_, {B, H, Dv}, type, dev, kLin);
+  TORCH_CHECK_VALUE(Hk > 0 && H > 0 && H % Hk == 0, "v's ", H, " heads must be a multiple of q's and k's ", Hk);
+  const bool per_row = a_.dim() != 1;
+  if (per_row) check("log_decay", a_, {B, H}, type, dev, kLin);
+  else check("log_decay", a_, {H}, type, dev, kLin);
+  TORCH_CHECK_VALUE(state.dim() == 4, "state must be a tensor (n, H, Dk, Dv)");
+  const int64_t n = state.size(0);
+  check("state", state, {n, H, Dk, Dv}, at::kFloat, dev, kLin);
+  TORCH_CHECK_VALUE(state.is_contiguous(), "state must be contiguous: it is updated in place");
+  Tensor slots = given(slots_);
+  if (slots.defined()) {
+    check("slots", slots, {B}, at::kInt, dev, kLin);
+    slots = slots.contiguous();
+  } else {
+    TORCH_CHECK_VALUE(n >= B, B, " rows need as many states, got ", n);
+  }
+  const Tensor q = rows(q_), k = rows(k_), v = rows(v_), a = a_.contiguous();
+  const c10::DeviceGuard guard(dev);
+  Tensor out = given(out_);
+  if (out.defined()) {
+    check("out", out, {B, H, Dv}, type, dev, kLin);
+    TORCH_CHECK_VALUE(out.is_contiguous(), "out must be contiguous");
+  } else {
+    out = at::empty({B, H, Dv}, q.options());
+  }
+  const bool dense = q.is_contiguous() && k.is_contiguous() && v.is_contiguous();
+  const int64_t strides[6] = {q.stride(0), q.stride(1), k.stride(0), k.stride(1), v.stride(0), v.stride(1)};
+  ok(gspn_linattn_step(ptr(q), ptr(k), ptr(v), ptr(a), fptr(state), static_cast<int32_t*>(ptr(slots)), ptr(out), n, B,
+                       H, Hk, Dk, Dv, dense ? nullptr : strides, dt, per_row ? GSPN_LINATTN_DECAY_PER_TOKEN : 0,
+                       (float)(scale ? *scale : 1.0 / std::sqrt((double)Dk)), stream_of(q)),
+     "gspn_linattn_step");
+  return out;
+}
+
+// ---------------------------------------------------------------------------
+// group norm
+// ---------------------------------------------------------------------------
+struct Norm {
+  Tensor x, w, b;  // contiguous; w, b may be undefined
+  int64_t B, L, C, G;
+  gspn_dtype dt;
+
+  Norm(const Tensor& x_, int64_t groups, const Tensor& w_, const Tensor& b_) : G(groups) {
+    check_gpu("x", x_, kNorm);
+    dt = dtype_of(x_, kNorm);
+    TORCH_CHECK_VALUE(x_.dim() >= 2, "x must be (B, ..., C), channels last");
+    B = x_.size(0);
+    C = x_.size(-1);
+    TORCH_CHECK_VALUE(G > 0 && C > 0 && C % G == 0, C, " channels do not make ", G, " groups");
+    L = 1;
+    for (int64_t i = 1; i + 1 < x_.dim(); ++i) L *= x_.size(i);
+    if (w_.defined()) check("weight", w_, {C}, x_.scalar_type(), x_.device(), kNorm);
+    if (b_.defined()) check("bias", b_, {C}, x_.scalar_type(), x_.device(), kNorm);
+    x = x_.contiguous();
+    w = w_.defined() ? w_.contiguous() : w_;
+    b = b_.defined() ? b_.contiguous() : b_;
+  }
+};
+
+// y, statistics (2, B, G)
+std::tuple<Tensor, Tensor> norm_fwd(const Norm& c, double eps, int64_t act) {
+  const c10::DeviceGuard guard(c.x.device());
+  Tensor y = at::empty(c.x.sizes(), c.x.options());
+  Tensor stats = at::empty({2, c.B, c.G}, c.x.options().dtype(at::kFloat));
+  const size_t need = gspn_group_norm_fwd_workspace_bytes(c.B, c.L, c.C, c.G, c.dt);
+  const Tensor ws = workspace(need, Tensor(), c.x);
+  float* mean = fptr(stats);
+  ok(gspn_group_norm_fwd(ptr(c.x), ptr(c.w), ptr(c.b), ptr(y), mean, mean ? mean + c.B * c.G : nullptr, c.B, c.L, c.C,
+                         c.G, (float)eps, (int)act, c.dt, ptr(ws), need, stream_of(c.x)),
+     "gspn_group_norm_fwd");
+  return {y, stats};
+}
+
+variable_list norm_bwd(const Norm& c, const Tensor& dy_, const float* mean, const float* rstd, int64_t act) {
+  const c10::DeviceGuard guard(c.x.device());
+  check("dy", dy_, c.x.sizes(), c.x.scalar_type(), c.x.device(), kNorm);
+  const Tensor dy = dy_.contiguous();
+  Tensor dx = at::empty(c.x.sizes(), c.x.options()), dw, db;
+  // an empty x leaves the parameters' gradients at zero
+  const auto param = [&] { return c.x.numel() ? at::empty({c.C}, c.x.options()) : at::zeros({c.C}, c.x.options()); };
+  if (c.w.defined()) dw = param();
+  if (c.b.defined()) db = param();
+  const size_t need = gspn_group_norm_bwd_workspace_bytes(c.B, c.L, c.C, c.G, c.dt);
+  const Tensor ws = workspace(need, Tensor(), c.x);
+  ok(gspn_group_norm_bwd(ptr(dy), ptr(c.x), ptr(c.w), ptr(c.b), mean, rstd, ptr(dx), ptr(dw), ptr(db), c.B, c.L, c.C,
+                         c.G, (int)act, c.dt, ptr(ws), need, stream_of(c.x)),
+     "gspn_group_norm_bwd");
+  return {dx, dw, db};
+}
+
+struct NormFn : torch::autograd::Function<NormFn> {
+  static Tensor forward(AutogradContext* ctx, const Tensor& x, const optional<Tensor>& w, const optional<Tensor>& b,
+                        int64_t groups, double eps, int64_t act) {
+    const Norm c(x, groups, given(w), given(b));
+    auto [y, stats] = norm_fwd(c, eps, act);
+    ctx->save_for_backward({c.x, c.w, c.b, stats});
+    ctx->saved_data["groups"] = groups;
+    ctx->saved_data["act"] = act;
+    return y;
+  }
+  static variable_list backward(AutogradContext* ctx, variable_list grads) {
+    const auto s = ctx->get_saved_variables();
+    const Norm c(s[0], ctx->saved_data["groups"].toInt(), s[1], s[2]);
+    const float* mean = fptr(s[3]);
+    variable_list out = norm_bwd(c, grads[0], mean, mean ? mean + c.B * c.G : nullptr, ctx->saved_data["act"].toInt());
+    out.resize(6);
+    return out;
+  }
+};
+
+// ---------------------------------------------------------------------------
+// the module
+// ---------------------------------------------------------------------------
+// without the interpreter's lock; a refusal becomes lib.GSPNError
+template <typename F> auto run(F f) {
+  try {
+    const py::gil_scoped_release unlocked;
+    return f();
+  } catch (const Refused& e) {
+    const py::object cls = py::reinterpret_borrow<py::object>(g_error);
+    const py::object ex = cls(e.status, e.where);
+    PyErr_SetObject(g_error, ex.ptr());
+    throw py::error_already_set();
+  }
+}
+py::object maybe(const Tensor& t) { return t.defined() ? py::cast(t) : py::none(); }
+template <typename F> void def(py::module_& m, const char* name, F f) { m.def(name, torch::wrap_pybind_function(f)); }
+
+}  // namespace
+
+PYBIND11_MODULE(_binding, m) {
+  m.def("set_error", [](py::object cls) { g_error = cls.release().ptr(); });
+  def(m, "linattn", [](const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& a, optional<double> scale,
+                       optional<Tensor> s0, bool return_state, optional<Tensor> cu) -> py::object {
+    const variable_list out = run([&] { return linattn(q, k, v, a, scale, s0, return_state, cu); });
+    return return_state ? py::object(py::make_tuple(out[0], out[1])) : py::cast(out[0]);
+  });
+  def(m, "linattn_fwd", [](const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& a, optional<double> scale,
+                           optional<Tensor> s0, bool return_state, optional<Tensor> cu, optional<Tensor> ws) {
+    const auto [o, sf, w] = run([&] {
+      const at::NoGradGuard no_grad;
+      return lin_fwd(Lin(q, k, v, a, scale, given(s0), given(cu)), return_state, given(ws));
+    });
+    return py::make_tuple(o, maybe(sf));
+  });
+  def(m, "linattn_workspace", [](const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& a,
+                                 optional<Tensor> cu) {
+    return run([&] {
+      const Lin c(q, k, v, a, std::nullopt, Tensor(), given(cu));
+      const Tensor ws = workspace(c.fwd_bytes(), Tensor(), c.q);
+      return ws.defined() ? ws : at::empty({0}, c.q.options().dtype(at::kByte));
+    });
+  });
+  def(m, "linattn_bwd", [](const Tensor& dout, const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& a,
+                           optional<double> scale, optional<Tensor> s0, optional<Tensor> dsf, optional<Tensor> cu,
+                           optional<Tensor> fws, optional<Tensor> ws) {
+    const variable_list g = run([&] {
+      const at::NoGradGuard no_grad;
+      return lin_bwd(Lin(q, k, v, a, scale, given(s0), given(cu)), dout, given(dsf), given(fws), given(ws));
+    });
+    return py::make_tuple(g[0], g[1], g[2], g[3], maybe(g[4]));
+  });
+  def(m, "linattn_step", [](const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& a, const Tensor& state,
+                            optional<double> scale, optional<Tensor> slots, optional<Tensor> out) {
+    return run([&] {
+      const at::NoGradGuard no_grad;
+      return linattn_step(q, k, v, a, state, scale, slots, out);
+    });
+  });
+  def(m, "group_norm", [](const Tensor& x, int64_t groups, optional<Tensor> w, optional<Tensor> b, double eps,
+                          int64_t act) { return run([&] { return NormFn::apply(x, w, b, groups, eps, act); }); });
+  def(m, "group_norm_fwd", [](const Tensor& x, int64_t groups, optional<Tensor> w, optional<Tensor> b, double eps,
+                              int64_t act) {
+    const auto [y, stats] = run([&] {
+      const at::NoGradGuard no_grad;
+      return norm_fwd(Norm(x, groups, given(w), given(b)), eps, act);
+    });
+    return py::make_tuple(y, stats.select(0, 0), stats.select(0, 1));
+  });
+  def(m, "group_norm_bwd", [](const Tensor& dy, const Tensor& x, const Tensor& mean, const Tensor& rstd,
+                              int64_t groups, optional<Tensor> w, optional<Tensor> b, int64_t act) {
+    const variable_list g = run([&] {
+      const at::NoGradGuard no_grad;
+      const Norm c(x, groups, given(w), given(b));
+      check("mean", mean, {c.B, c.G}, at::kFloat, c.x.device(), kNorm);
+      check("rstd", rstd, {c.B, c.G}, at::kFloat, c.x.device(), kNorm);
+      const Tensor mu = mean.contiguous(), rs = rstd.contiguous();
+      return norm_bwd(c, dy, fptr(mu), fptr(rs), act);
+    });
+    return py::make_tuple(g[0], maybe(g[1]), maybe(g[2]));
+  });
+}

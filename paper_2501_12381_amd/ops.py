@@ -24,9 +24,8 @@ from functools import lru_cache
 import torch
 
 from . import lib as L
-from .seq import (GSPNGroupNorm, GSPNLinAttn, gspn_group_norm, gspn_group_norm_bwd,  # noqa: F401
-                  gspn_group_norm_fwd, gspn_linattn, gspn_linattn_bwd, gspn_linattn_fwd, gspn_linattn_step,
-                  gspn_linattn_workspace)
+from .seq import (gspn_group_norm, gspn_group_norm_bwd, gspn_group_norm_fwd, gspn_linattn,  # noqa: F401
+                  gspn_linattn_bwd, gspn_linattn_fwd, gspn_linattn_step, gspn_linattn_workspace)
 
 _DT = {torch.float32: L.GSPN_F32, torch.bfloat16: L.GSPN_BF16}
 
