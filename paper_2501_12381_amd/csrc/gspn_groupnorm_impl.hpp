@@ -137,43 +137,57 @@ __global__ void __launch_bounds__(NT < 256 ? 256 : NT) gn_team_fwd_kernel(Args A
     w[j] = m.on ? param<T>(A.weight, ch + j, 1.f) : 0.f;
     bias[j] = m.on ? param<T>(A.bias, ch + j, 0.f) : 0.f;
   }
-  for (int64_t b = m.b0; b < m.b1; b += R) {
-    float v[R][K][V], p[R];
+  // the next entries' values are asked for before this round's are worked on
+  Pack<T, V> ahead[R][K];
+  const auto ask = [&](int64_t b) {
 #pragma unroll
     for (int i = 0; i < R; ++i) {
       const int64_t bi = min(b + i, m.b1 - 1);  // entries past the last are computed again and not stored
-      const T* x = reinterpret_cast<const T*>(A.x) + bi * A.L * A.C;
-      p[i] = to_f(x[m.g * cpg]);
+      const T* x = reinterpret_cast<const T*>(A.x) + bi * A.L * A.C + ch;
 #pragma unroll
-      for (int k = 0; k < K; ++k) {
-        if (m.has(k, A.L)) load_v<T, V>(x + (int64_t)(m.r0 + k * m.RT) * A.C + ch, v[i][k]);
-        else
-#pragma unroll
-          for (int j = 0; j < V; ++j) v[i][k][j] = p[i];
-      }
+      for (int k = 0; k < K; ++k)
+        if (m.has(k, A.L)) ahead[i][k] = *reinterpret_cast<const Pack<T, V>*>(x + (int64_t)(m.r0 + k * m.RT) * A.C);
     }
+  };
+  if (m.b0 < m.b1) ask(m.b0);
+  for (int64_t b = m.b0; b < m.b1; b += R) {
+    float v[R][K][V], mu[R], rs[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      // sums go around the slab's first value
+      float p;
+      if constexpr (NT == 64) p = __shfl(to_f(ahead[i][0].e[0]), threadIdx.x & 63 & ~(LP - 1));
+      else p = to_f(reinterpret_cast<const T*>(A.x)[(b + i) * A.L * A.C + m.g * cpg]);
+      mu[i] = p;
+#pragma unroll
+      for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[i][k][j] = m.has(k, A.L) ? to_f(ahead[i][k].e[j]) : p;
+    }
+    if (R > 1 || K == 1)
+      if (b + R < m.b1) ask(b + R);
 #pragma unroll
     for (int i = 0; i < R; ++i) {
       float s = 0.f, q = 0.f;
 #pragma unroll
       for (int k = 0; k < K; ++k)
 #pragma unroll
-        for (int j = 0; j < V; ++j) s += v[i][k][j] - p[i];
-      const float mean = p[i] + team_sum<NT>(s, LP, red) * inv_m;
+        for (int j = 0; j < V; ++j) s += v[i][k][j] - mu[i];
+      mu[i] += team_sum<NT>(s, LP, red) * inv_m;
       // the values are here: the squares go around the mean itself
 #pragma unroll
       for (int k = 0; k < K; ++k)
         if (m.has(k, A.L))
 #pragma unroll
           for (int j = 0; j < V; ++j) {
-            const float d = v[i][k][j] - mean;
+            const float d = v[i][k][j] - mu[i];
             q = __builtin_fmaf(d, d, q);
           }
-      const float rstd = rsqrtf(team_sum<NT>(q, LP, red) * inv_m + A.eps);
+      rs[i] = rsqrtf(team_sum<NT>(q, LP, red) * inv_m + A.eps);
       if (b + i < m.b1) {
-        if (m.t == 0) {
-          A.mean[(b + i) * A.G + m.g] = mean;
-          A.rstd[(b + i) * A.G + m.g] = rstd;
+        if (R == 1 && m.t == 0) {
+          A.mean[b * A.G + m.g] = mu[0];
+          A.rstd[b * A.G + m.g] = rs[0];
         }
         T* y = reinterpret_cast<T*>(A.y) + (b + i) * A.L * A.C + ch;
 #pragma unroll
@@ -181,11 +195,26 @@ __global__ void __launch_bounds__(NT < 256 ? 256 : NT) gn_team_fwd_kernel(Args A
           if (m.has(k, A.L)) {
             float o[V];
 #pragma unroll
-            for (int j = 0; j < V; ++j) o[j] = act_f(__builtin_fmaf((v[i][k][j] - mean) * rstd, w[j], bias[j]), A.act);
+            for (int j = 0; j < V; ++j) o[j] = act_f(__builtin_fmaf((v[i][k][j] - mu[i]) * rs[i], w[j], bias[j]), A.act);
             store_v<T, V>(y + (int64_t)(m.r0 + k * m.RT) * A.C, o);
           }
       }
     }
+    if constexpr (R > 1) {
+      // lane i of the team (or its only lane, entry by entry) stores entry i's statistics
+      for (int i = m.t; i < R; i += LP)
+        if (m.t < LP && b + i < m.b1) {
+          float mean = mu[0], rstd = rs[0];
+#pragma unroll
+          for (int j = 1; j < R; ++j) {
+            mean = i == j ? mu[j] : mean;
+            rstd = i == j ? rs[j] : rstd;
+          }
+          A.mean[(b + i) * A.G + m.g] = mean;
+          A.rstd[(b + i) * A.G + m.g] = rstd;
+        }
+    }
+    if (R == 1 && K > 1 && b + R < m.b1) ask(b + R);
   }
 }
 
@@ -203,30 +232,43 @@ __global__ void __launch_bounds__(NT < 256 ? 256 : NT) gn_team_bwd_kernel(Args A
     bias[j] = m.on && A.act ? param<T>(A.bias, ch + j, 0.f) : 0.f;
     aw[j] = ab[j] = 0.f;
   }
-  for (int64_t b = m.b0; b < m.b1; b += R) {
-    float xh[R][K][V], dz[R][K][V], mean[R], rstd[R];
+  Pack<T, V> nx[R][K], nd[R][K];
+  float nm[R], nr[R];
+  const auto ask = [&](int64_t b) {
 #pragma unroll
     for (int i = 0; i < R; ++i) {
       const int64_t bi = min(b + i, m.b1 - 1);
-      const bool live = b + i < m.b1;
-      mean[i] = A.mean[bi * A.G + m.g];
-      rstd[i] = A.rstd[bi * A.G + m.g];
+      nm[i] = A.mean[bi * A.G + m.g];
+      nr[i] = A.rstd[bi * A.G + m.g];
       const T *x = reinterpret_cast<const T*>(A.x) + bi * A.L * A.C + ch,
               *dy = reinterpret_cast<const T*>(A.dy) + bi * A.L * A.C + ch;
 #pragma unroll
-      for (int k = 0; k < K; ++k) {
-        if (m.has(k, A.L) && live) {
-          load_v<T, V>(x + (int64_t)(m.r0 + k * m.RT) * A.C, xh[i][k]);
-          load_v<T, V>(dy + (int64_t)(m.r0 + k * m.RT) * A.C, dz[i][k]);
-        } else {
+      for (int k = 0; k < K; ++k)
+        if (m.has(k, A.L)) {
+          nx[i][k] = *reinterpret_cast<const Pack<T, V>*>(x + (int64_t)(m.r0 + k * m.RT) * A.C);
+          nd[i][k] = *reinterpret_cast<const Pack<T, V>*>(dy + (int64_t)(m.r0 + k * m.RT) * A.C);
+        }
+    }
+  };
+  if (m.b0 < m.b1) ask(m.b0);
+  for (int64_t b = m.b0; b < m.b1; b += R) {
+    float xh[R][K][V], dz[R][K][V], rstd[R];
 #pragma unroll
-          for (int j = 0; j < V; ++j) {
-            xh[i][k][j] = mean[i];
-            dz[i][k][j] = 0.f;
-          }
+    for (int i = 0; i < R; ++i) {
+      rstd[i] = nr[i];
+      const float off = -nm[i] * nr[i];
+      const bool live = b + i < m.b1;
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        const bool has = m.has(k, A.L) && live;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          xh[i][k][j] = has ? __builtin_fmaf(to_f(nx[i][k].e[j]), nr[i], off) : 0.f;
+          dz[i][k][j] = has ? to_f(nd[i][k].e[j]) : 0.f;
         }
       }
     }
+    if (K == 1 && b + R < m.b1) ask(b + R);
 #pragma unroll
     for (int i = 0; i < R; ++i) {
       float s1 = 0.f, s2 = 0.f;
@@ -234,7 +276,6 @@ __global__ void __launch_bounds__(NT < 256 ? 256 : NT) gn_team_bwd_kernel(Args A
       for (int k = 0; k < K; ++k)
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-          xh[i][k][j] = (xh[i][k][j] - mean[i]) * rstd[i];
           if (A.act) dz[i][k][j] *= act_slope(__builtin_fmaf(xh[i][k][j], w[j], bias[j]), A.act);
           ab[j] += dz[i][k][j];
           aw[j] = __builtin_fmaf(dz[i][k][j], xh[i][k][j], aw[j]);
@@ -256,6 +297,7 @@ __global__ void __launch_bounds__(NT < 256 ? 256 : NT) gn_team_bwd_kernel(Args A
           }
       }
     }
+    if (K > 1 && b + R < m.b1) ask(b + R);
   }
   // sums over the team's RT rows, channel by channel
   float* out = reinterpret_cast<float*>(A.ws) + m.b0 / rows * 2 * A.C + m.g * cpg;
