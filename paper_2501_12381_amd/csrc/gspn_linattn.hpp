@@ -134,8 +134,10 @@ struct StepArgs {
 };
 hipError_t linattn_step(const StepArgs& a);
 
-// register-order size of a state, in elements (sides padded to 64 or 128)
-__host__ __device__ constexpr int pad_dim(int d) { return d <= 64 ? 64 : 128; }
+// a state's side in the kernels: 32 where both sides are, else 64 or 128
+__host__ __device__ constexpr int pad_dim(int d, int other) {
+  return d <= 32 && other <= 32 ? 32 : d <= 64 ? 64 : 128;
+}
 inline int chunk_len(int dtype) { return dtype == 0 ? 32 : 64; }
 constexpr int kMaxDim = 128;
 

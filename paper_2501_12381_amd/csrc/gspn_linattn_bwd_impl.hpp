@@ -311,7 +311,9 @@ template <typename T, int KP, int VP> hipError_t linattn_bwd_launch(const BwdArg
 }
 
 template <typename T> hipError_t linattn_bwd_t(const BwdArgs& a) {
-  const bool kw = a.g.Dk > 64, vw = a.g.Dv > 64;
+  const int kp = pad_dim(a.g.Dk, a.g.Dv), vp = pad_dim(a.g.Dv, a.g.Dk);
+  const bool kw = kp == 128, vw = vp == 128;
+  if (kp == 32) return linattn_bwd_launch<T, 32, 32>(a);
   if (kw && vw) return linattn_bwd_launch<T, 128, 128>(a);
   if (kw) return linattn_bwd_launch<T, 128, 64>(a);
   if (vw) return linattn_bwd_launch<T, 64, 128>(a);

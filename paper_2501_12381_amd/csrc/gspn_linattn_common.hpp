@@ -429,53 +429,59 @@ __device__ __forceinline__ void decayed(const Decays<T>& d, const float* raw, fl
 }
 
 // The products of a chunk's token pairs, decayed: out[t][s] = (a_s . b_t) scale
-// e^{G_t - G_s} for s <= t, 0 above; the work of `waves` waves, of which this is
-// number `wave`.  Three of four quarters of the C x C table: bf16 quarters are 32 x 32
-// tiles, and the one above the diagonal is never read; fp32 ones are 16 x 16
-// (a quarter of the time of one wave's 32 x 32 tile), and the fourth is zeros.
+// e^{G_t - G_s} for s <= t, 0 above, in quarters of the C x C table: 0 (t, s in the
+// first half), 1 (t in the second, s in the first), 2 (both in the second).  bf16
+// quarters are 32 x 32 tiles, and the one above the diagonal is never read; fp32
+// ones are 16 x 16 (a quarter of the time of one wave's 32 x 32 tile), and the
+// fourth, tile 3, is zeros.
+template <typename T, int DP>
+__device__ __forceinline__ void pair_tile(const Decays<T>& d, const T* a, const T* b, int stride, float scale, T* out,
+                                          int ostride, int tile, int lane) {
+  constexpr int Q = Elem<T>::kChunk / 2;
+  const int tt = tile == 3 ? 0 : (tile + 1) >> 1, st = tile == 3 ? 1 : tile >> 1;
+  if constexpr (sizeof(T) == 2) {
+    const int h = lane >> 5, l = pl(lane & 31);
+    f32x16 acc = {};
+#pragma unroll
+    for (int k0 = 0; k0 < DP; k0 += 16)
+      Elem<T>::mma(acc, row_frag(a, stride, Q * st + l, k0, h), row_frag(b, stride, Q * tt + l, k0, h));
+    const int t = Q * tt + l;
+#pragma unroll
+    for (int r = 0; r < 16; r += 8) {
+      const int s = Q * st + reg_line(r, h);
+      float raw[8], x[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) raw[j] = acc[r + j];
+      if (tile == 1) decayed<T, 8, false>(d, raw, scale, t, s, x);
+      else decayed<T, 8, true>(d, raw, scale, t, s, x);
+      Elem<T>::store8(out + t * ostride + s, x);
+    }
+  } else {
+    typedef float f32x4 __attribute__((ext_vector_type(4)));
+    const int l = lane & 15, q = lane >> 4, t = Q * tt + l, s = Q * st + 4 * q;
+    float x[4] = {0.f, 0.f, 0.f, 0.f};
+    if (tile < 3) {
+      f32x4 acc = {};
+#pragma unroll
+      for (int k0 = 0; k0 < DP; k0 += 32) {
+        const auto fa = Elem<T>::row(a + (Q * st + l) * stride + k0 + 8 * q),
+                   fb = Elem<T>::row(b + (Q * tt + l) * stride + k0 + 8 * q);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(fa.v[j], fb.v[j], acc, 0, 0, 0);
+      }
+      const float raw[4] = {acc[0], acc[1], acc[2], acc[3]};
+      if (tile == 1) decayed<T, 4, false>(d, raw, scale, t, s, x);
+      else decayed<T, 4, true>(d, raw, scale, t, s, x);
+    }
+    *reinterpret_cast<float4*>(out + t * ostride + s) = make_float4(x[0], x[1], x[2], x[3]);
+  }
+}
+// the whole table, by `waves` waves of which this is number `wave`
 template <typename T, int DP>
 __device__ __forceinline__ void pair_table(const Decays<T>& d, const T* a, const T* b, int stride, float scale, T* out,
                                            int ostride, int wave, int waves, int lane) {
-  constexpr int Q = Elem<T>::kChunk / 2;
-  for (int tile = wave; tile < (sizeof(T) == 2 ? 3 : 4); tile += waves) {
-    const int tt = tile == 3 ? 0 : (tile + 1) >> 1, st = tile == 3 ? 1 : tile >> 1;  // (t, s): 00, 10, 11, (01)
-    if constexpr (sizeof(T) == 2) {
-      const int h = lane >> 5, l = pl(lane & 31);
-      f32x16 acc = {};
-#pragma unroll
-      for (int k0 = 0; k0 < DP; k0 += 16)
-        Elem<T>::mma(acc, row_frag(a, stride, Q * st + l, k0, h), row_frag(b, stride, Q * tt + l, k0, h));
-      const int t = Q * tt + l;
-#pragma unroll
-      for (int r = 0; r < 16; r += 8) {
-        const int s = Q * st + reg_line(r, h);
-        float raw[8], x[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) raw[j] = acc[r + j];
-        if (tile == 1) decayed<T, 8, false>(d, raw, scale, t, s, x);
-        else decayed<T, 8, true>(d, raw, scale, t, s, x);
-        Elem<T>::store8(out + t * ostride + s, x);
-      }
-    } else {
-      typedef float f32x4 __attribute__((ext_vector_type(4)));
-      const int l = lane & 15, q = lane >> 4, t = Q * tt + l, s = Q * st + 4 * q;
-      float x[4] = {0.f, 0.f, 0.f, 0.f};
-      if (tile < 3) {
-        f32x4 acc = {};
-#pragma unroll
-        for (int k0 = 0; k0 < DP; k0 += 32) {
-          const auto fa = Elem<T>::row(a + (Q * st + l) * stride + k0 + 8 * q),
-                     fb = Elem<T>::row(b + (Q * tt + l) * stride + k0 + 8 * q);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(fa.v[j], fb.v[j], acc, 0, 0, 0);
-        }
-        const float raw[4] = {acc[0], acc[1], acc[2], acc[3]};
-        if (tile == 1) decayed<T, 4, false>(d, raw, scale, t, s, x);
-        else decayed<T, 4, true>(d, raw, scale, t, s, x);
-      }
-      *reinterpret_cast<float4*>(out + t * ostride + s) = make_float4(x[0], x[1], x[2], x[3]);
-    }
-  }
+  for (int tile = wave; tile < (sizeof(T) == 2 ? 3 : 4); tile += waves)
+    pair_tile<T, DP>(d, a, b, stride, scale, out, ostride, tile, lane);
 }
 
 // ---------------------------------------------------------------------------

@@ -14,17 +14,28 @@
 namespace gspn {
 namespace la {
 
+// Waves of a workgroup.  One for each 32 columns of v; heads of up to 32 would leave
+// one wave to do everything in turn, so in bf16 two share the tokens (the first and
+// the second 32 of the chunk): each forms its own rows of P and o and keeps the whole
+// state.
+template <typename T, int VP> struct FwdWaves {
+  static constexpr int kHalves = VP == 32 && sizeof(T) == 2 ? 2 : 1;
+  static constexpr int kThreads = 2 * VP * kHalves;
+};
+
 // EXACT: the final state is returned
 template <typename T, int KP, int VP, bool EXACT>
-__global__ void __launch_bounds__(2 * VP, 2) linattn_fwd_kernel(FwdArgs A) {
+__global__ void __launch_bounds__((FwdWaves<T, VP>::kThreads), 2) linattn_fwd_kernel(FwdArgs A) {
   using E = Elem<T>;
-  constexpr int C = E::kChunk, NT = 2 * VP, NW = VP / 32, NC = C / 32;
+  constexpr int NH = FwdWaves<T, VP>::kHalves, NT = FwdWaves<T, VP>::kThreads, NW = NT / 64;
+  constexpr int C = E::kChunk, NC = C / 32, NO = NC / NH;  // NO: 32-token tiles of this wave
   constexpr int KS = E::stride(KP), VS = E::stride(VP), PS = E::stride(C);
   __shared__ __align__(16) T sq[C * KS], sk[C * KS], sv[C * VS], sp[C * PS];
   __shared__ Decays<T> decs[2];  // this chunk's and the next one's
 
   const Geom& g = A.g;
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, h = lane >> 5, l = pl(lane & 31), c0 = 32 * wave;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, h = lane >> 5, l = pl(lane & 31), c0 = 32 * (wave / NH);
+  const int first_tile = NH == 2 ? wave : 0;
   int pi, head;
   if (!find_work(g, blockIdx.x, pi, head)) return;
   const Piece pc = find_piece(g, pi);
@@ -39,7 +50,7 @@ __global__ void __launch_bounds__(2 * VP, 2) linattn_fwd_kernel(FwdArgs A) {
   f32x16 S[KP / 32];
   const int64_t sidx = ((int64_t)pc.seq * g.H + head) * g.Dk * g.Dv;
   if (pc.first) state_read<KP>(S, A.s0 ? A.s0 + sidx : nullptr, g.Dk, g.Dv, g.Dv, 1, c0 + l, h);
-  else state_read_regs<KP>(S, A.start + ((int64_t)pi * g.H + head) * (KP * VP), wave, lane);
+  else state_read_regs<KP>(S, A.start + ((int64_t)pi * g.H + head) * (KP * VP), wave / NH, lane);
 
   const T* a = reinterpret_cast<const T*>(A.a) + head +
                (A.per_token ? (pc.batch * g.T + pc.t0) * (int64_t)g.H : (int64_t)0);
@@ -80,41 +91,52 @@ __global__ void __launch_bounds__(2 * VP, 2) linattn_fwd_kernel(FwdArgs A) {
       ask(t0 + 2 * C);
     }
 
-    pair_table<T, KP>(dec, sk, sq, KS, A.scale, sp, PS, wave, NW, lane);  // P[t][s]
+    // P[t][s]
+    if constexpr (NH == 2) {
+      if (wave == 0) pair_tile<T, KP>(dec, sk, sq, KS, A.scale, sp, PS, 0, lane);
+      else
+        for (int tile = 1; tile < 3; ++tile) pair_tile<T, KP>(dec, sk, sq, KS, A.scale, sp, PS, tile, lane);
+    } else {
+      pair_table<T, KP>(dec, sk, sq, KS, A.scale, sp, PS, wave, NW, lane);
+    }
     __builtin_amdgcn_sched_barrier(0);
     // o^T = S^T q^T e^G: lines of v along the registers, lane = t
-    f32x16 acc[NC];
+    f32x16 acc[NO];
 #pragma unroll
-    for (int tt = 0; tt < NC; ++tt) acc[tt] = f32x16{};
+    for (int i = 0; i < NO; ++i) acc[i] = f32x16{};
 #pragma unroll
     for (int kk = 0; kk < KP / 16; ++kk) {
       const auto sf = reg_frag<T>(S, kk);
 #pragma unroll
-      for (int tt = 0; tt < NC; ++tt) E::mma(acc[tt], sf, row_frag(sq, KS, 32 * tt + l, 16 * kk, h));
+      for (int i = 0; i < NO; ++i) E::mma(acc[i], sf, row_frag(sq, KS, 32 * (first_tile + i) + l, 16 * kk, h));
     }
 #pragma unroll
-    for (int tt = 0; tt < NC; ++tt) acc[tt] *= dec.qf[32 * tt + l];
+    for (int i = 0; i < NO; ++i) acc[i] *= dec.qf[32 * (first_tile + i) + l];
     __builtin_amdgcn_sched_barrier(0);
     state_add<T, KP, EXACT>(S, sk, KS, sv, VS, c0, dec.kf, dec.tot, lane);
-    lds_barrier();
+    if constexpr (NH == 1) lds_barrier();  // else a wave reads the rows of P that it wrote
     // + v^T P^T
 #pragma unroll
     for (int k0 = 0; k0 < C; k0 += 16) {
+      if (NH == 2 && k0 / 32 > first_tile) continue;
       const auto vf = col_frag(sv, VS, k0, c0, lane);
 #pragma unroll
-      for (int tt = k0 / 32; tt < NC; ++tt) E::mma(acc[tt], vf, row_frag(sp, PS, 32 * tt + l, k0, h));
+      for (int i = 0; i < NO; ++i)
+        if (NH == 2 || k0 / 32 <= i) E::mma(acc[i], vf, row_frag(sp, PS, 32 * (first_tile + i) + l, k0, h));
     }
 #pragma unroll
-    for (int tt = 0; tt < NC; ++tt)
-      if (t0 + 32 * tt + l < pc.len) put_lines(orow + 32 * tt * ot, acc[tt], g.Dv - c0, A.ovec, h);
+    for (int i = 0; i < NO; ++i) {
+      const int t = 32 * (first_tile + i);
+      if (t0 + t + l < pc.len) put_lines(orow + t * ot, acc[i], g.Dv - c0, A.ovec, h);
+    }
     orow += C * ot;
     lds_barrier();
   }
-  if (EXACT && pc.last) state_write<KP>(S, A.sf + sidx, g.Dk, g.Dv, g.Dv, 1, c0 + l, h);
+  if (EXACT && pc.last && first_tile == 0) state_write<KP>(S, A.sf + sidx, g.Dk, g.Dv, g.Dv, 1, c0 + l, h);
 }
 
 template <typename T, int KP, int VP> hipError_t linattn_fwd_launch(const FwdArgs& a) {
-  const dim3 grid(work_grid(a.g)), block(2 * VP);
+  const dim3 grid(work_grid(a.g)), block(FwdWaves<T, VP>::kThreads);
   const hipStream_t st = (hipStream_t)a.stream;
   if (a.sf) hipLaunchKernelGGL((linattn_fwd_kernel<T, KP, VP, true>), grid, block, 0, st, a);
   else hipLaunchKernelGGL((linattn_fwd_kernel<T, KP, VP, false>), grid, block, 0, st, a);
@@ -122,7 +144,9 @@ template <typename T, int KP, int VP> hipError_t linattn_fwd_launch(const FwdArg
 }
 
 template <typename T> hipError_t linattn_fwd_t(const FwdArgs& a) {
-  const bool kw = a.g.Dk > 64, vw = a.g.Dv > 64;
+  const int kp = pad_dim(a.g.Dk, a.g.Dv), vp = pad_dim(a.g.Dv, a.g.Dk);
+  const bool kw = kp == 128, vw = vp == 128;
+  if (kp == 32) return linattn_fwd_launch<T, 32, 32>(a);
   if (kw && vw) return linattn_fwd_launch<T, 128, 128>(a);
   if (kw) return linattn_fwd_launch<T, 128, 64>(a);
   if (vw) return linattn_fwd_launch<T, 64, 128>(a);

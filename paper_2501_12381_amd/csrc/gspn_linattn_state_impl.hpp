@@ -110,7 +110,9 @@ template <typename T, int XP, int YP> hipError_t linattn_state_launch(const Stat
 }
 
 template <typename T> hipError_t linattn_state_one(const StateArgs& a, const StateArgs* b) {
-  const bool xw = a.Dx > 64, yw = a.Dy > 64;
+  const int xp = pad_dim(a.Dx, a.Dy), yp = pad_dim(a.Dy, a.Dx);
+  const bool xw = xp == 128, yw = yp == 128;
+  if (xp == 32) return linattn_state_launch<T, 32, 32>(a, b);
   if (xw && yw) return linattn_state_launch<T, 128, 128>(a, b);
   if (xw) return linattn_state_launch<T, 128, 64>(a, b);
   if (yw) return linattn_state_launch<T, 64, 128>(a, b);
@@ -118,7 +120,7 @@ template <typename T> hipError_t linattn_state_one(const StateArgs& a, const Sta
 }
 
 template <typename T> hipError_t linattn_state_t(const StateArgs& a, const StateArgs* b) {
-  if (b && (pad_dim(a.Dx) != pad_dim(b->Dx) || pad_dim(a.Dy) != pad_dim(b->Dy))) {  // other tiles: two launches
+  if (b && pad_dim(a.Dx, a.Dy) != pad_dim(b->Dx, b->Dy)) {  // other tiles: two launches
     const hipError_t e = linattn_state_one<T>(a, nullptr);
     return e == hipSuccess ? linattn_state_one<T>(*b, nullptr) : e;
   }

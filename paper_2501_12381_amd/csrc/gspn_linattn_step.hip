@@ -102,7 +102,7 @@ __global__ void __launch_bounds__(256) linattn_join_kernel(JoinArgs A0, JoinArgs
   const bool two = (int)blockIdx.x >= second;
   const JoinArgs& A = two ? A1 : A0;
   const Geom& g = A.g;
-  const int block = (int)blockIdx.x - (two ? second : 0), XP = pad_dim(A.Dx), YP = pad_dim(A.Dy);
+  const int block = (int)blockIdx.x - (two ? second : 0), XP = pad_dim(A.Dx, A.Dy), YP = pad_dim(A.Dy, A.Dx);
   const int parts = XP * YP / 1024, nh = block / parts, head = nh % g.H, n = nh / g.H;
   int first, last;  // piece indexes
   if (g.cu) {
@@ -214,7 +214,7 @@ hipError_t linattn_step(const StepArgs& a) { return a.dtype == 0 ? step_t<float>
 
 hipError_t linattn_join(const JoinArgs& a, const JoinArgs* b) {
   const auto blocks = [](const JoinArgs& j) {
-    return (int64_t)(pad_dim(j.Dx) * pad_dim(j.Dy) / 1024) * j.g.N * j.g.H;
+    return (int64_t)(pad_dim(j.Dx, j.Dy) * pad_dim(j.Dy, j.Dx) / 1024) * j.g.N * j.g.H;
   };
   const int64_t n = blocks(a), all = n + (b ? blocks(*b) : 0);
   hipLaunchKernelGGL(linattn_join_kernel, dim3((unsigned)all), dim3(256), 0, (hipStream_t)a.stream, a, b ? *b : a,

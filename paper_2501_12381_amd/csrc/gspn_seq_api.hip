@@ -57,10 +57,11 @@ struct Lin {
 // idle.  `room` is how many workgroups of the call's main kernel the card holds at
 // once (256 compute units, by LDS and registers); a cut costs a walk of the
 // states and their join, about what half a main walk does.
-//   whole sequences: from 192 (sequence, head) pairs on; from 128 on with head sizes
-//   over 64 and less than 24 chunks; under 6 chunks.  Forward / backward in us, whole against
-//   cut: 256 pairs x 16 chunks of 128 values 69/198, 127/322; 128 x 16 60/155, 73/166;
-//   192 x 13 chunks of 64 46/96, 49/105; 120 x 32 88/203, 54/118; 64 x 8 39/72, 31/64.
+//   whole sequences: from 192 (sequence, head) pairs on (384 with head sizes up to 32;
+//   in bf16 128 with head sizes over 64 and less than 24 chunks); under 6 chunks.
+//   Forward / backward in us, whole against cut: bf16 256 pairs x 16 chunks of 128
+//   values 69/198, 127/322; 128 x 16 60/155, 73/166; 120 x 32 of 64 88/203, 54/118; 64 x 8
+//   39/72, 31/64; 192 x 13 of 32 36/92, 34/67; fp32 128 x 32 of 128 208/596, 180/452.
 //   else as many pieces as there is room for, down to one chunk: a second round of
 //   workgroups costs more than longer pieces (64 pairs x 64 chunks of 128, forward with 512
 //   workgroups 94, with 1024 113; backward with 256 335, with 512 346).
@@ -68,8 +69,10 @@ struct Lin {
 // states that the forward left.
 int64_t piece_chunks(const Lin* p, bool bwd) {
   const int64_t T = p->T, C = p->C, n = (T + C - 1) / C, pairs = p->N * p->H;
-  const bool wide = p->KP > 64 || p->VP > 64;
-  const int64_t room = bwd ? (wide ? 256 : 512) : (p->VP > 64 ? 512 : 1024);
+  const bool wide = p->KP > 64 || p->VP > 64, small = p->VP == 32, f32 = p->dtype == GSPN_F32;
+  const int64_t room = bwd ? (small ? (f32 ? 1024 : 768) : wide ? 256 : 512)
+                           : (small && f32 ? 1536 : p->VP > 64 ? 512 : 1024);
+  const bool whole = n < 6 || pairs >= (small ? 384 : 192) || (wide && !f32 && pairs >= 128 && n < 24) || pairs == 0;
   int64_t L = n > 0 ? n : 1;  // chunks of a piece
   if (p->packed) {
     // pieces end at multiples of L tokens of the packed axis and at the sequences' ends
@@ -77,7 +80,7 @@ int64_t piece_chunks(const Lin* p, bool bwd) {
     if (blocks < room / (2 * p->H)) blocks = room / (2 * p->H);
     if (blocks < 1) blocks = 1;
     L = (n + blocks - 1) / blocks;
-  } else if (n >= 6 && pairs < 192 && !(wide && pairs >= 128 && n < 24) && pairs > 0) {
+  } else if (!whole) {
     const int64_t P = room / pairs;
     L = (n + P - 1) / P;
   }
@@ -118,8 +121,8 @@ int check_lin(int64_t n_seq, int64_t B, int64_t T, int64_t H, int64_t Hk, int64_
       !mul_ok(n, 128 * 128 * 4, &n))
     return GSPN_ERR_SHAPE;
   *p = Lin{B, T, n_seq, (int)H, (int)Hk, (int)Dk, (int)Dv, dtype, flags, packed, {}, 0, 0, 0};
-  p->KP = la::pad_dim(p->Dk);
-  p->VP = la::pad_dim(p->Dv);
+  p->KP = la::pad_dim(p->Dk, p->Dv);
+  p->VP = la::pad_dim(p->Dv, p->Dk);
   p->C = la::chunk_len(dtype);
   if (n_seq == 0 && !packed) return GSPN_OK;
   make_geom(p, cu, bwd);
