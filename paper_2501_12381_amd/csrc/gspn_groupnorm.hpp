@@ -57,7 +57,7 @@ struct Plan {
 // tensors; 16 waves of a team share a SIMD's registers by four)
 constexpr int team_loads(int V, int NT, bool bwd) {
   const int n = 64 / (bwd ? 2 : 1) / (NT == 1024 ? 2 : 1) / V;
-  const int most = NT == 1024 ? 8 : 16;
+  const int most = NT == 1024 && (bwd || V > 2) ? 8 : 16;
   return n < most ? n : most;
 }
 
