@@ -12,6 +12,11 @@ and projects back to `dim` channels.
 
 The 1x1 convolutions are plain GEMMs and run through PyTorch's library
 kernels; every step of the scan and its adjoint runs in the HIP kernels.
+
+RasterMixer is the layer's one-dimensional relative: the map's tokens in raster
+order, mixed by linear attention with an input-dependent decay for each head, with
+the channels-last norms around it.  It trains on maps, takes prompts, and generates
+token by token from a carried state.
 """
 from __future__ import annotations
 
@@ -51,3 +56,71 @@ class GSPNModule(nn.Module):
                            logits=True, renorm=self.edge_renorm, y_per_dir=True)  # (n, B, C, H, W)
         B, C, H, W = x.shape
         return self.merge(ys.permute(1, 0, 2, 3, 4).reshape(B, self.n * C, H, W))
+
+
+class RasterMixer(nn.Module):
+    """x + out(norm_heads(linear_attention(proj(act(norm(x)))))) over a map's raster.
+
+    x is channels last: (B, H, W, C), or (B, T, C) for tokens as they come.  The
+    first norm takes its statistics over the map (`per_token` False: the layer of a
+    diffusion or classification model) or over each token's groups (`per_token` True:
+    what a model that generates tokens in order needs); the second one is over each
+    head of each token."""
+
+    def __init__(self, dim: int, heads: int, head_dim: int, kv_heads: int | None = None,
+                 value_dim: int | None = None, groups: int = 32, per_token: bool = False, eps: float = 1e-5):
+        super().__init__()
+        self.heads, self.qk_heads = heads, heads if kv_heads is None else kv_heads
+        self.head_dim, self.value_dim = head_dim, head_dim if value_dim is None else value_dim
+        self.groups, self.per_token, self.eps = groups, per_token, eps
+        if self.qk_heads < 1 or heads % self.qk_heads:
+            raise ValueError(f"{heads} heads must be a multiple of kv_heads, got {kv_heads}")
+        if dim % groups:
+            raise ValueError(f"{dim} channels do not make {groups} groups")
+        self.widths = (self.qk_heads * head_dim, self.qk_heads * head_dim, heads * self.value_dim, heads)
+        self.norm_weight, self.norm_bias = nn.Parameter(torch.ones(dim)), nn.Parameter(torch.zeros(dim))
+        self.proj = nn.Linear(dim, sum(self.widths))
+        self.head_weight = nn.Parameter(torch.ones(heads * self.value_dim))
+        self.head_bias = nn.Parameter(torch.zeros(heads * self.value_dim))
+        self.out = nn.Linear(heads * self.value_dim, dim)
+        with torch.no_grad():  # memories of about ten to a thousand tokens: e^a = sigmoid(bias)
+            self.proj.bias[-heads:] = torch.linspace(2.2, 6.9, heads)
+
+    def _split(self, tokens, lead):
+        """q, k, v (views of the projection, not copied) and the log decay of tokens (n, C)."""
+        q, k, v, a = self.proj(tokens).split(self.widths, dim=-1)
+        return (q.view(*lead, self.qk_heads, self.head_dim), k.view(*lead, self.qk_heads, self.head_dim),
+                v.view(*lead, self.heads, self.value_dim),
+                nn.functional.logsigmoid(a).view(*lead, self.heads))
+
+    def _merge(self, x, o):
+        y = ops.gspn_group_norm(o.reshape(-1, self.heads * self.value_dim), self.heads, self.head_weight,
+                                self.head_bias, eps=self.eps)
+        return x + self.out(y).view(x.shape)
+
+    def _norm(self, x, alone: bool):
+        x = x.reshape(-1, x.shape[-1]) if alone else x
+        return ops.gspn_group_norm(x, self.groups, self.norm_weight, self.norm_bias, eps=self.eps, act="silu")
+
+    def new_state(self, n: int) -> torch.Tensor:
+        """Empty states of n sequences."""
+        return torch.zeros((n, self.heads, self.head_dim, self.value_dim), device=self.proj.weight.device)
+
+    def forward(self, x, state=None, return_state: bool = False, cu_seqlens=None):
+        """The layer's output, and with return_state the states behind the last tokens.
+        cu_seqlens: prompts packed into one row (B = 1), as in gspn_linattn."""
+        B, C = x.shape[0], x.shape[-1]
+        lead = (B, x.numel() // (B * C) if x.numel() else 0)
+        q, k, v, a = self._split(self._norm(x, self.per_token).reshape(-1, C), lead)
+        o = ops.gspn_linattn(q, k, v, a, initial_state=state, return_state=return_state, cu_seqlens=cu_seqlens)
+        if return_state:
+            return self._merge(x, o[0]), o[1]
+        return self._merge(x, o)
+
+    @torch.no_grad()
+    def step(self, x, state, slots=None):
+        """One token of each of B sequences, x (B, C): the layer's output; `state` moves on in place."""
+        if not self.per_token:
+            raise ValueError("single tokens need per_token norms: a map's statistics are not known before its end")
+        q, k, v, a = self._split(self._norm(x, True), x.shape[:1])
+        return self._merge(x, ops.gspn_linattn_step(q, k, v, a, state, slots=slots))
