@@ -91,10 +91,13 @@ inline Plan make_plan(int64_t B, int64_t L, int C, int G, int dtype, int vec, bo
   }
   if (p.team) {
     // the parameters are read, and in the backward a partial sum is written, once
-    // for all of a team's entries: as many as leave two waves a SIMD
+    // for all of a team's entries: as many as leave four waves a SIMD, in the
+    // backward two (16384 tokens x 16 heads of 128: forward 60, 38, 31, 35 us with 1024,
+    // 2048, 4096 and 8192 waves or more; backward with its sums 55, 49, 56, 63 us
+    // with 1024, 2048, 512 and 4096)
     p.rows = 1;
     const int64_t waves = p.NT == 64 ? (slabs * p.LP + 63) / 64 : slabs * (p.NT / 64);
-    while (p.rows < 64 && waves / (2 * p.rows) >= 2048) p.rows *= 2;
+    while (p.rows < 64 && waves / (2 * p.rows) >= (bwd ? 2048 : 4096)) p.rows *= 2;
     return p;
   }
   p.V = full;
