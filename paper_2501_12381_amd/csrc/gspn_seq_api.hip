@@ -66,7 +66,7 @@ struct Lin {
 //   workgroups costs more than longer pieces (64 pairs x 64 chunks of 128, forward with 512
 //   workgroups 94, with 1024 113; backward with 256 335, with 512 346).
 // A backward's piece is a whole number of the forward's pieces: it starts from the
-// states that the forward left.
+// states that the forward left (the number above, or for packed ones the nearest).
 int64_t piece_chunks(const Lin* p, bool bwd) {
   const int64_t T = p->T, C = p->C, n = (T + C - 1) / C, pairs = p->N * p->H;
   const bool wide = p->KP > 64 || p->VP > 64, small = p->VP == 32, f32 = p->dtype == GSPN_F32;
@@ -75,9 +75,15 @@ int64_t piece_chunks(const Lin* p, bool bwd) {
   const bool whole = n < 6 || pairs >= (small ? 384 : 192) || (wide && !f32 && pairs >= 128 && n < 24) || pairs == 0;
   int64_t L = n > 0 ? n : 1;  // chunks of a piece
   if (p->packed) {
-    // pieces end at multiples of L tokens of the packed axis and at the sequences' ends
-    int64_t blocks = room / p->H - p->N;
-    if (blocks < room / (2 * p->H)) blocks = room / (2 * p->H);
+    // pieces end at multiples of L tokens of the packed axis and at the sequences'
+    // ends: the ends count as pieces too, down to half of the cuts.  The backward's
+    // short ones fit between the others unless there is nothing else to do (12
+    // sequences of 0 to 2307 tokens, 16 heads of 128: 189 us so, 261 with half the cuts;
+    // one of 8192: 182 with 16, 155 with 15); where the sequences fill the card the
+    // long ones alone are cut (64 of 50 to 600: 349 and 331).
+    int64_t blocks = room / p->H;
+    if (pairs >= room) blocks /= 2;
+    else if (!bwd || 4 * pairs < room) blocks = blocks - p->N > blocks / 2 ? blocks - p->N : blocks / 2;
     if (blocks < 1) blocks = 1;
     L = (n + blocks - 1) / blocks;
   } else if (!whole) {
@@ -87,7 +93,7 @@ int64_t piece_chunks(const Lin* p, bool bwd) {
   if (L < 1) L = 1;
   if (bwd) {
     const int64_t f = piece_chunks(p, false);
-    if (f < n) L = (L + f - 1) / f * f;
+    if (f < n) L = (L + (p->packed && L >= f ? f / 2 : f - 1)) / f * f;
   }
   return L;
 }
