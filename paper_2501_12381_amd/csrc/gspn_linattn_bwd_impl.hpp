@@ -141,7 +141,7 @@ __global__ void __launch_bounds__(2 * (KP + VP), 2) linattn_bwd_kernel(BwdArgs A
   rk.init(head_rows<T>(A.k, pc, hk), A.k, g.Dk, from, tid);
   rv.init(head_rows<T>(A.v, pc, head), A.v, g.Dv, from, tid);
   rg.init(head_rows<T>(A.dout, pc, head), A.dout, g.Dv, from, tid);
-  double ra = 0.0;
+  T ra = from_f<T>(0.f);
   const auto load = [&](int t) {
     const int left = pc.len - t;
     rq.load(left, A.q, -1);

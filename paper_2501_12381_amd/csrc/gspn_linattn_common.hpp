@@ -341,10 +341,14 @@ template <typename T> struct Decays {
   int pad;
 };
 
+// a token's log decay as it stands in memory (converted where it is used: at the load,
+// the conversion would wait for it)
 template <typename T>
-__device__ __forceinline__ double load_decay(const T* __restrict__ a, int64_t stride, int t, int rows) {
-  if (t >= rows) return 0.0;
-  const double g = (double)to_f(a[t * stride]) * 1.4426950408889634;
+__device__ __forceinline__ T load_decay(const T* __restrict__ a, int64_t stride, int t, int rows) {
+  return t < rows ? a[t * stride] : from_f<T>(0.f);
+}
+template <typename T> __device__ __forceinline__ double log2_decay(T a) {
+  const double g = (double)to_f(a) * 1.4426950408889634;
   return g < -150.0 ? -150.0 : g;
 }
 
@@ -383,10 +387,10 @@ template <int LANE> __device__ __forceinline__ double from_lane(double v) {
   return __longlong_as_double(((long long)hi << 32) | (unsigned)lo);
 }
 
-// one wave; g: lane t's own term (0 past the chunk).  Returns G_C.
-template <typename T> __device__ __forceinline__ double chunk_decays(Decays<T>& d, double g, float scale, int lane) {
+// one wave; a: lane t's own log decay (0 past the chunk).  Returns G_C.
+template <typename T> __device__ __forceinline__ double chunk_decays(Decays<T>& d, T a, float scale, int lane) {
   constexpr int C = Elem<T>::kChunk;
-  g = prefix_sum(g);
+  const double g = prefix_sum(log2_decay(a));
   const double all = lane_63(g), g0 = from_lane<0>(g), g1 = from_lane<C / 2>(g);
   const double own = g - (lane < C / 2 ? g0 : g1);
   const bool small = own < 64.0 && own > -64.0;  // lanes past the chunk repeat its last token's G

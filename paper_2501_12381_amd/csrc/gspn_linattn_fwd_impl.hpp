@@ -60,7 +60,7 @@ __global__ void __launch_bounds__((FwdWaves<T, VP>::kThreads), 2) linattn_fwd_ke
   rq.init(head_rows<T>(A.q, pc, hk), A.q, g.Dk, 0, tid);
   rk.init(head_rows<T>(A.k, pc, hk), A.k, g.Dk, 0, tid);
   rv.init(head_rows<T>(A.v, pc, head), A.v, g.Dv, 0, tid);
-  double ra = 0.0;
+  T ra = from_f<T>(0.f);
   const auto load = [&](int t) {
     const int left = pc.len - t;
     rq.load(left, A.q, 1);

@@ -55,7 +55,8 @@ __global__ void __launch_bounds__(2 * YP, 2) linattn_state_kernel(StateArgs A0, 
   const int n = (pc.len + C - 1) / C, dir = A.reverse ? -1 : 1, from = A.reverse && n > 0 ? (n - 1) * C : 0;
   rx.init(head_rows<T>(A.x, pc, A.x_shared ? hk : head), A.x, A.Dx, from, tid);
   ry.init(head_rows<T>(A.y, pc, A.y_shared ? hk : head), A.y, A.Dy, from, tid);
-  double ra = 0.0, all = 0.0;
+  T ra = from_f<T>(0.f);
+  double all = 0.0;
   const auto load = [&](int t) {
     const int left = pc.len - t;
     rx.load(left, A.x, dir);
