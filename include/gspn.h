@@ -267,8 +267,9 @@ int gspn_scan_bwd(const void* dy, const void* x, const void* w, const void* lam,
  * Arithmetic: sums, decays and states in fp32 (exponents in 64 bits).  With bf16
  * tensors the state is rounded to bf16 where it meets q, and products of q and k
  * where they meet v (as operands of matrix instructions); what is added to a
- * state is not rounded.  A non-finite value of a token reaches the outputs of the
- * up to 64 tokens of its chunk, earlier ones of the same sequence too.
+ * state is not rounded.  Infinities and NaN reach the outputs that the formula has
+ * them in, as one or the other, and no earlier token's or other sequence's; gradients they may
+ * reach within the up to 64 tokens of their chunk, earlier ones too.
  * Results repeat bit for bit.
  * ------------------------------------------------------------------------- */
 enum { GSPN_LINATTN_DECAY_PER_TOKEN = 1u };

@@ -19,6 +19,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "gspn_device.hpp"
 #include "gspn_linattn.hpp"
 
@@ -310,6 +312,41 @@ template <typename T, int DP, int NT> struct Stage {
       }
     }
     p += dir * (C * rows.st);
+  }
+  // one of the values is infinite or not a number
+  __device__ __forceinline__ bool odd() const {
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    using W = typename std::conditional<sizeof(T) == 2, u16x2, uint32_t>::type;
+    W most = {};
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const uint32_t w[4] = {r[i].x, r[i].y, r[i].z, r[i].w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t x = w[j] & (sizeof(T) == 2 ? 0x7fff7fffu : 0x7fffffffu);
+        most = __builtin_elementwise_max(most, __builtin_bit_cast(W, x));
+      }
+    }
+    if constexpr (sizeof(T) == 2) return (most[0] > most[1] ? most[0] : most[1]) >= 0x7f80;
+    else return most >= 0x7f800000u;
+  }
+  // zeroes those values; first[column]: the first row of the chunk that has one (C: none)
+  __device__ __forceinline__ void drop_odd(int* first) {
+    constexpr int N = 4 / (int)sizeof(T);  // values of a word
+    constexpr uint32_t kInf = sizeof(T) == 2 ? 0x7f80u : 0x7f800000u, kMask = sizeof(T) == 2 ? 0xffffu : ~0u;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      uint32_t w[4] = {r[i].x, r[i].y, r[i].z, r[i].w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+          if ((w[j] >> (16 * k) & kInf) == kInf) {
+            w[j] &= ~(kMask << (16 * k));
+            atomicMin(first + opaque(c) + j * N + k, opaque(row) + i * kRows);
+          }
+      r[i] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
   }
   __device__ __forceinline__ void store(T* tile) const {
 #pragma unroll

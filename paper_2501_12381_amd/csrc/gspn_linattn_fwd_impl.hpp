@@ -32,6 +32,10 @@ __global__ void __launch_bounds__((FwdWaves<T, VP>::kThreads), 2) linattn_fwd_ke
   constexpr int KS = E::stride(KP), VS = E::stride(VP), PS = E::stride(C);
   __shared__ __align__(16) T sq[C * KS], sk[C * KS], sv[C * VS], sp[C * PS];
   __shared__ Decays<T> decs[2];  // this chunk's and the next one's
+  // The products below the diagonal are zeros, but zero times infinity is not: infinities
+  // and NaN of v are zeros in LDS, and what the formula has them in is NaN.  Columns'
+  // first tokens with one, and whether there is any, in this chunk and the next.
+  __shared__ int odd_from[2][VP], odd[2];
 
   const Geom& g = A.g;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, h = lane >> 5, l = pl(lane & 31), c0 = 32 * (wave / NH);
@@ -72,22 +76,33 @@ __global__ void __launch_bounds__((FwdWaves<T, VP>::kThreads), 2) linattn_fwd_ke
   const auto ask = [&](int t) {
     if (wave == NW - 1 && lane < C) ra = load_decay(a + t * at, at, lane, pc.len - t);
   };
+  if (tid < VP) odd_from[0][tid] = C;
+  if (tid == 0) odd[0] = 0;
   if (pc.len > 0) {
     load(0);
     ask(0);
     if (wave == NW - 1) chunk_decays(decs[0], ra, A.scale, lane);
     ask(C);
   }
+  lds_barrier();
   T* orow = o + l * ot + c0;
   for (int t0 = 0; t0 < pc.len; t0 += C) {
+    const int now = t0 / C & 1;
     rq.store(sq);
     rk.store(sk);
+    if (rv.odd()) {
+      rv.drop_odd(odd_from[now]);
+      odd[now] = 1;
+    }
     rv.store(sv);
-    const Decays<T>& dec = decs[t0 / C & 1];
+    const Decays<T>& dec = decs[now];
     lds_barrier();
+    const int any_odd = __builtin_amdgcn_readfirstlane(odd[now]);
+    if (tid < VP) odd_from[now ^ 1][tid] = C;
+    if (tid == 0) odd[now ^ 1] = 0;
     if (t0 + C < pc.len) {
       load(t0 + C);
-      if (wave == NW - 1) chunk_decays(decs[(t0 / C + 1) & 1], ra, A.scale, lane);
+      if (wave == NW - 1) chunk_decays(decs[now ^ 1], ra, A.scale, lane);
       ask(t0 + 2 * C);
     }
 
@@ -123,6 +138,20 @@ __global__ void __launch_bounds__((FwdWaves<T, VP>::kThreads), 2) linattn_fwd_ke
 #pragma unroll
       for (int i = 0; i < NO; ++i)
         if (NH == 2 || k0 / 32 <= i) E::mma(acc[i], vf, row_frag(sp, PS, 32 * (first_tile + i) + l, k0, h));
+    }
+    if (any_odd) {
+      const float nan = __builtin_nanf("");
+      const bool bad = odd_from[now][c0 + l] < C;
+#pragma unroll
+      for (int m = 0; m < KP / 32; ++m)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) S[m][r] = bad ? nan : S[m][r];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int from = odd_from[now][c0 + reg_line(r, h)];
+#pragma unroll
+        for (int i = 0; i < NO; ++i) acc[i][r] = 32 * (first_tile + i) + l >= from ? nan : acc[i][r];
+      }
     }
 #pragma unroll
     for (int i = 0; i < NO; ++i) {

@@ -126,6 +126,28 @@ def test_tokens_of_no_sequence(per_token, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("dims", [(32, 32), (24, 40), (64, 64), (128, 64), (128, 128)], ids=str)
+@pytest.mark.parametrize("name,T", [("v", 200), ("k", 200), ("q", 200), ("a", 200), ("v", 1100)])
+def test_non_finite_values_and_earlier_tokens(name, T, dims, dtype):
+    """Infinities and NaN of a token reach the outputs that the formula has them in, and no earlier one."""
+    print(f"{name} T {T} dims {dims} {dtype}", flush=True)
+    d = inputs(1, T, 2, 2, *dims, dtype, True, 1, False, seed=T)
+    at = (0, T - 10, 0) if name == "a" else (0, T - 10, 0, 3)
+    d[name][at] = float("nan")
+    at = (0, T - 130, 1) if name == "a" else (0, T - 130, 1, 5)
+    d[name][at] = float("inf") if name == "v" else float("nan")
+    o, _ = ops.gspn_linattn_fwd(d["q"], d["k"], d["v"], d["a"])
+    h = {k: np64(d[k]) for k in ("q", "k", "v", "a")}
+    with np.errstate(invalid="ignore"):
+        ref = R.linattn(h["q"], h["k"], h["v"], h["a"], dims[0] ** -0.5, None, None, None, None)[0]
+    got, fine = np64(o), np.isfinite(ref)
+    assert fine[:, :T - 130].all() and not fine.all()
+    np.testing.assert_array_equal(np.isfinite(got), fine)
+    close(torch.from_numpy(got[fine]), ref[fine], dtype, "finite part")
+
+
+@pytest.mark.gpu
 def test_sequences_do_not_touch():
     """Non-finite values of one sequence stay in it."""
     cu = [0, 40, 80, 120]
