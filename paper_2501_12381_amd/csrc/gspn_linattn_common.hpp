@@ -255,8 +255,9 @@ __device__ __forceinline__ Piece find_piece(const Geom& g, int i) {
   p.batch = 0;
   p.first = b == b0;
   p.last = b == b1;
-  p.t0 = max(s, b * g.L);
-  p.len = b < b0 || b > b1 ? -1 : max(0, min(e, (b + 1) * g.L) - p.t0);
+  const int64_t at = (int64_t)b * g.L;  // the last piece may reach past 32 bits
+  p.t0 = (int)max((int64_t)s, at);
+  p.len = b < b0 || b > b1 ? -1 : max(0, (int)min((int64_t)e, at + g.L) - p.t0);
   return p;
 }
 
