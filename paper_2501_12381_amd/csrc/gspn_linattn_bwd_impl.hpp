@@ -16,7 +16,7 @@
 // formula, q.dq - k.dk summed from the sequence's end, adds up the rounding of
 // every later token.
 //
-// Two kinds of waves: VP/32 own 32 lines of v each (P, dv, dM), KP/32 own 32
+// Kinds of waves: VP/32 own 32 lines of v each (P, dv, dM), KP/32 own 32
 // lines of k each (Z, dq, dk).  P, Z and dM (rounded to the element type) pass
 // through LDS.  What bounds it: bytes (q, k, v, do and a state in, dq, dk, dv out),
 // then the chain of a chunk: 4 sequences of 4096 tokens, 16 heads of 128, 4 of q and k,
@@ -79,13 +79,26 @@ __device__ __forceinline__ void put_part(int16_t* p, float* scale, const f32x16&
   scale[h] = (most + bad) * (1.f / 32767.f);
 }
 
+// Waves of a workgroup: one for each 32 lines of v and of k, and for heads of up to 32,
+// which have one of each, two more that form P and the decays, and Z (without and with
+// them, 32 x 784 tokens, 6 heads: bf16 74 and 69 us, fp32 107 and 98; 128 x 512, 8 heads:
+// bf16 132 and 104, fp32 183 and 165).  kPerSimd: waves that a SIMD's registers are to
+// hold; fp32's need four, for as many workgroups as without helpers (else 238 us, not 165).
+template <typename T, int KP, int VP> struct BwdWaves {
+  static constexpr int kHelp = VP == 32 ? 2 : 0;
+  static constexpr int kThreads = 2 * (KP + VP) + 64 * kHelp;
+  static constexpr int kPerSimd = VP == 32 && sizeof(T) == 4 ? 4 : 2;
+};
+
 // EXACT: the gradient of the initial states is returned
 template <typename T, int KP, int VP, bool EXACT>
-__global__ void __launch_bounds__(2 * (KP + VP), 2) linattn_bwd_kernel(BwdArgs A) {
+__global__ void __launch_bounds__((BwdWaves<T, KP, VP>::kThreads), (BwdWaves<T, KP, VP>::kPerSimd))
+    linattn_bwd_kernel(BwdArgs A) {
   using E = Elem<T>;
   using Lds = BwdLds<T, KP, VP>;
   constexpr int C = E::kChunk, NC = C / 32;
-  constexpr int NA = VP / 32, NB = KP / 32, NT = 64 * (NA + NB);
+  constexpr int NA = VP / 32, NB = KP / 32, NT = BwdWaves<T, KP, VP>::kThreads;
+  constexpr bool kHelp = BwdWaves<T, KP, VP>::kHelp > 0;
   constexpr int KS = Lds::KS, VS = Lds::VS, PS = Lds::PS;
   extern __shared__ __align__(16) unsigned char lds_raw[];
   Lds& s = *reinterpret_cast<Lds*>(lds_raw);
@@ -132,6 +145,7 @@ __global__ void __launch_bounds__(2 * (KP + VP), 2) linattn_bwd_kernel(BwdArgs A
   const int hk = head / (g.H / g.Hk);
   const bool va = wave < NA;               // this wave owns columns of v (else of k)
   const int c0 = 32 * (va ? wave : wave - NA), wb = wave - NA;
+  const bool help = kHelp && wave >= NA + NB;
   const int64_t sidx = ((int64_t)pc.seq * g.H + head) * g.Dk * g.Dv;
   const T* a = reinterpret_cast<const T*>(A.a) + head + (A.per_token ? row0 * g.H : (int64_t)0);
   const int64_t at = A.per_token ? g.H : 0;
@@ -151,9 +165,9 @@ __global__ void __launch_bounds__(2 * (KP + VP), 2) linattn_bwd_kernel(BwdArgs A
     rv.load(left, A.v, -1);
     rg.load(left, A.dout, -1);
   };
-  // the decays are the work of the last of the waves that own columns of v, which
-  // has none of the pairs: summed a chunk ahead, asked for two ahead
-  const bool decays = wave == NA - 1;
+  // the decays are the work of a helper, or of the last of the waves that own columns
+  // of v, which has none of the pairs: summed a chunk ahead, asked for two ahead
+  const bool decays = wave == (kHelp ? NA + NB : NA - 1);
   const auto ask = [&](int c) {
     if (decays && lane < C && c >= 0) ra = load_decay(a + (int64_t)c * C * at, at, lane, pc.len - c * C);
   };
@@ -169,34 +183,47 @@ __global__ void __launch_bounds__(2 * (KP + VP), 2) linattn_bwd_kernel(BwdArgs A
     if (decays) chunk_decays(s.dec[(n - 1) & 1], ra, A.scale, lane);
     ask(n - 2);
   }
-  // the two kinds of waves run loops of their own (the registers of the one are
+  float da_sum = 0.f;  // with one decay for the head
+  // a chunk's da, from what the other waves left of it: suffix sums of f, prefix sums of w
+  const auto finish = [&](int c) {
+    const int e = c & 1;
+    float f = 0.f, w = 0.f, x = 0.f;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) x += s.x[e][b];
+    if (lane < C) {
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        f += s.f[e][b][lane];
+        w += s.w[e][b][lane];
+      }
+    }
+    const float fp = prefix_sum(f), wp = prefix_sum(w);
+    const float r = (lane_63(fp) - (fp - f)) + (wp - w) + s.dec[e].tot * x;
+    const int t = c * C + lane;
+    if (lane < C && t < pc.len) {
+      if (A.per_token) da[(int64_t)t * g.H] = from_f<T>(r);
+      else da_sum += r;
+    }
+  };
+  // the decays' wave in chunk c, once the chunk's rows and the last chunk's sums are in LDS
+  const auto next_decays = [&](int c) {
+    if (c + 1 < n) finish(c + 1);  // whose decays' place the next chunk's take
+    if (c > 0) chunk_decays(s.dec[(c - 1) & 1], ra, A.scale, lane);
+    ask(c - 2);
+  };
+  const auto last_decays = [&] {
+    if (n > 0) finish(0);
+    if (!A.per_token) {
+      da_sum = lane_63(prefix_sum(da_sum));
+      if (lane == 0) A.da_piece[slot] = da_sum;
+    }
+  };
+  // the kinds of waves run loops of their own (the registers of the one are
   // then not kept through the other's code), with the same barriers
   if (va) {
     f32x16 M[KP / 32];
     if (pc.last) state_read<KP>(M, A.dsf ? A.dsf + sidx : nullptr, g.Dk, g.Dv, g.Dv, 1, c0 + l, h);
     else state_read_regs<KP>(M, A.end + slot * (KP * VP), wave, lane);
-    float da_sum = 0.f;  // with one decay for the head
-    // a chunk's da, from what the other waves left of it: suffix sums of f, prefix sums of w
-    const auto finish = [&](int c) {
-      const int e = c & 1;
-      float f = 0.f, w = 0.f, x = 0.f;
-#pragma unroll
-      for (int b = 0; b < NB; ++b) x += s.x[e][b];
-      if (lane < C) {
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-          f += s.f[e][b][lane];
-          w += s.w[e][b][lane];
-        }
-      }
-      const float fp = prefix_sum(f), wp = prefix_sum(w);
-      const float r = (lane_63(fp) - (fp - f)) + (wp - w) + s.dec[e].tot * x;
-      const int t = c * C + lane;
-      if (lane < C && t < pc.len) {
-        if (A.per_token) da[(int64_t)t * g.H] = from_f<T>(r);
-        else da_sum += r;
-      }
-    };
     for (int c = n - 1; c >= 0; --c) {
       const int t0 = c * C;
       stage();
@@ -206,12 +233,10 @@ __global__ void __launch_bounds__(2 * (KP + VP), 2) linattn_bwd_kernel(BwdArgs A
       lds_barrier();
       const Decays<T>& dec = s.dec[c & 1];
       if (c > 0) load(t0 - C);
-      if (decays) {
-        if (c + 1 < n) finish(c + 1);  // whose decays' place the next chunk's take
-        if (c > 0) chunk_decays(s.dec[(c - 1) & 1], ra, A.scale, lane);
-        ask(c - 2);
+      if (!kHelp) {
+        if (decays) next_decays(c);
+        pair_table<T, KP>(dec, s.k, s.q, KS, A.scale, s.p, PS, wave, NA, lane);  // P[t][s]
       }
-      pair_table<T, KP>(dec, s.k, s.q, KS, A.scale, s.p, PS, wave, NA, lane);  // P[t][s]
       __builtin_amdgcn_sched_barrier(0);
       // dv^T = dM^T k^T e^{G_C - G_s}
       f32x16 acc[NC];
@@ -242,12 +267,24 @@ __global__ void __launch_bounds__(2 * (KP + VP), 2) linattn_bwd_kernel(BwdArgs A
       }
       lds_barrier();
     }
-    if (decays && n > 0) finish(0);
+    if (decays) last_decays();
     if (EXACT && pc.first) state_write<KP>(M, A.ds0 + sidx, g.Dk, g.Dv, g.Dv, 1, c0 + l, h);
-    if (!A.per_token && decays) {
-      da_sum = lane_63(prefix_sum(da_sum));
-      if (lane == 0) A.da_piece[slot] = da_sum;
+  } else if (help) {
+    for (int c = n - 1; c >= 0; --c) {
+      stage();
+      lds_barrier();
+      const Decays<T>& dec = s.dec[c & 1];
+      if (c > 0) load(c * C - C);
+      if (decays) {
+        pair_table<T, KP>(dec, s.k, s.q, KS, A.scale, s.p, PS, 0, 1, lane);  // P[t][s]
+        next_decays(c);
+      } else {
+        pair_table<T, VP>(dec, s.v, s.g, VS, A.scale, s.z, PS, 0, 1, lane);  // Z[t][s]
+      }
+      lds_barrier();
+      lds_barrier();
     }
+    if (decays) last_decays();
   } else {
     const T* chunks = reinterpret_cast<const T*>(A.chunks) + ((int64_t)pi * (g.L / C) * g.H + head) * (KP * VP) +
                       (wb * (VP / 16) * 64 + lane) * 8;
@@ -267,7 +304,7 @@ __global__ void __launch_bounds__(2 * (KP + VP), 2) linattn_bwd_kernel(BwdArgs A
       lds_barrier();
       const Decays<T>& dec = s.dec[c & 1];
       if (c > 0) load(t0 - C);
-      pair_table<T, VP>(dec, s.v, s.g, VS, A.scale, s.z, PS, wb, NB, lane);  // Z[t][s]
+      if (!kHelp) pair_table<T, VP>(dec, s.v, s.g, VS, A.scale, s.z, PS, wb, NB, lane);  // Z[t][s]
       __builtin_amdgcn_sched_barrier(0);
       // the terms through the states: dq^T = S do^T scale e^{G_t}, dk^T = dM v^T e^{G_C - G_s}
       f32x16 aq[NC], ak[NC];
@@ -347,7 +384,7 @@ template <typename T, int KP, int VP, bool EXACT> hipError_t linattn_bwd_start(c
   const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
                                            hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(kernel, dim3(work_grid(a.g)), dim3(2 * (KP + VP)), bytes, (hipStream_t)a.stream, a);
+  hipLaunchKernelGGL(kernel, dim3(work_grid(a.g)), dim3((BwdWaves<T, KP, VP>::kThreads)), bytes, (hipStream_t)a.stream, a);
   return hipGetLastError();
 }
 template <typename T, int KP, int VP> hipError_t linattn_bwd_launch(const BwdArgs& a) {

@@ -14,11 +14,18 @@
 namespace gspn {
 namespace la {
 
+// Waves: one for each 32 lines of y; for sides of up to 32 another one forms the decays
+// (32 x 784 tokens, 6 heads, bf16, gradients: 69 us without it, 64 with).
+template <int YP> struct StateWaves {
+  static constexpr int kHelp = YP == 32 ? 1 : 0;
+  static constexpr int kThreads = 2 * YP + 64 * kHelp;
+};
+
 template <typename T, int XP, int YP, bool EXACT>
-__global__ void __launch_bounds__(2 * YP, 2) linattn_state_kernel(StateArgs A0, StateArgs A1, int second) {
+__global__ void __launch_bounds__(StateWaves<YP>::kThreads, 2) linattn_state_kernel(StateArgs A0, StateArgs A1, int second) {
   const bool two = (int)blockIdx.x >= second;  // the second of two walks
   const StateArgs& A = two ? A1 : A0;
-  constexpr int C = Elem<T>::kChunk, NT = 2 * YP;
+  constexpr int C = Elem<T>::kChunk, NT = StateWaves<YP>::kThreads;
   constexpr int XS = Elem<T>::stride(XP), YS = Elem<T>::stride(YP);
   __shared__ __align__(16) T sx[C * XS], sy[C * YS];
   __shared__ Decays<T> decs[2];  // this chunk's and the next one's
@@ -32,8 +39,10 @@ __global__ void __launch_bounds__(2 * YP, 2) linattn_state_kernel(StateArgs A0, 
   if (A.mode == 0 && (A.reverse ? pc.first : pc.last)) return;  // nobody reads its state
   const int hk = head / (g.H / g.Hk), yc = 32 * wave + l;
   const int64_t slot = (int64_t)pi * g.H + head;
+  const bool help = StateWaves<YP>::kHelp && wave >= YP / 32;
+  const bool decays = wave == (StateWaves<YP>::kHelp ? YP / 32 : 0);
   f32x16 S[XP / 32];
-  if (A.mode == 0) {
+  if (A.mode == 0 || help) {
 #pragma unroll
     for (int m = 0; m < XP / 32; ++m) S[m] = f32x16{};
   } else if (pc.first) {
@@ -64,13 +73,13 @@ __global__ void __launch_bounds__(2 * YP, 2) linattn_state_kernel(StateArgs A0, 
     ry.load(left, A.y, dir);
   };
   const auto ask = [&](int t) {  // two chunks ahead
-    if (wave == 0 && lane < C && t >= 0) ra = load_decay(a + t * at, at, lane, pc.len - t);
+    if (decays && lane < C && t >= 0) ra = load_decay(a + t * at, at, lane, pc.len - t);
   };
   T* chunks = reinterpret_cast<T*>(A.chunks);
   if (n > 0) {
     load(from);
     ask(from);
-    if (wave == 0) all += chunk_decays(decs[0], ra, A.scale, lane);
+    if (decays) all += chunk_decays(decs[0], ra, A.scale, lane);
     ask(from + dir * C);
   }
   for (int i = 0; i < n; ++i) {
@@ -81,27 +90,27 @@ __global__ void __launch_bounds__(2 * YP, 2) linattn_state_kernel(StateArgs A0, 
     lds_barrier();
     if (i + 1 < n) {
       load((c + dir) * C);
-      if (wave == 0) all += chunk_decays(decs[(i + 1) & 1], ra, A.scale, lane);
+      if (decays) all += chunk_decays(decs[(i + 1) & 1], ra, A.scale, lane);
       ask((c + 2 * dir) * C);
     }
-    if (A.mode == 1) {
+    if (A.mode == 1 && !help) {
       T* out = chunks + (((int64_t)pi * (g.L / C) + c) * g.H + head) * (XP * YP) + (wave * (XP / 16) * 64 + lane) * 8;
 #pragma unroll
       for (int kk = 0; kk < XP / 16; ++kk)
         *reinterpret_cast<typename Elem<T>::Frag*>(out + kk * 512) = reg_frag<T>(S, kk);
     }
-    state_add<T, XP, EXACT>(S, sx, XS, sy, YS, 32 * wave, A.reverse ? dec.qf : dec.kf, dec.tot, lane);
+    if (!help) state_add<T, XP, EXACT>(S, sx, XS, sy, YS, 32 * wave, A.reverse ? dec.qf : dec.kf, dec.tot, lane);
     lds_barrier();
   }
   if (A.mode == 0) {
-    state_write_regs<XP>(S, A.local + slot * (XP * YP), wave, lane);
-    if (tid == 0) A.gtot[slot] = exp2_wide(all);
+    if (!help) state_write_regs<XP>(S, A.local + slot * (XP * YP), wave, lane);
+    if (decays && lane == 0) A.gtot[slot] = exp2_wide(all);
   }
 }
 
 template <typename T, int XP, int YP> hipError_t linattn_state_launch(const StateArgs& a, const StateArgs* b) {
   const int n = (int)work_grid(a.g);
-  const dim3 grid((unsigned)(b ? 2 * n : n)), block(2 * YP);
+  const dim3 grid((unsigned)(b ? 2 * n : n)), block(StateWaves<YP>::kThreads);
   const hipStream_t st = (hipStream_t)a.stream;
   // fp32 products keep all bits anyway
   if ((a.exact || (b && b->exact)) && sizeof(T) == 2)
