@@ -20,7 +20,7 @@
 // lines of k each (Z, dq, dk).  P, Z and dM (rounded to the element type) pass
 // through LDS.  What bounds it: bytes (q, k, v, do and a state in, dq, dk, dv out),
 // then the chain of a chunk: 4 sequences of 4096 tokens, 16 heads of 128, 4 of q and k,
-// bf16 take 150 us for 510 MB, 3.4 TB/s, with one workgroup of 8 waves a compute unit
+// bf16 take 147 us for 510 MB, 3.5 TB/s, with one workgroup of 8 waves a compute unit
 // (142 KB of LDS), half of the waves' time waiting and the matrix units busy for a sixth.
 #pragma once
 

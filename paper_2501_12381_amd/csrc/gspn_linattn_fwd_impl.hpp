@@ -1,8 +1,8 @@
 // Linear attention, forward: one workgroup walks one piece of one head.
 //
 // What bounds it: with enough workgroups the bytes of q, k, v and o, each moved once
-// (one sequence of 65536 tokens, 10 heads of 64, bf16: 336 MB in 70 us, 4.8 TB/s; 512 heads
-// x 1024 tokens of 128: 537 MB in 134 us); with about one a compute unit the chain of
+// (one sequence of 65536 tokens, 10 heads of 64, bf16: 336 MB in 72 us, 4.7 TB/s; 512 heads
+// x 1024 tokens of 128: 537 MB in 137 us); with about one a compute unit the chain of
 // a chunk (128 heads of that: 65 us for a quarter of the bytes; the matrix units are
 // busy a fifth of the time, and a third of the waves' time is waiting).
 // Split: wave w owns columns 32w..32w+31 of v, o and the state, so the state

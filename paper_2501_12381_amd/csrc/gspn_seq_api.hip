@@ -64,7 +64,9 @@ struct Lin {
 //   39/72, 31/64; 192 x 13 of 32 36/92, 34/67; fp32 128 x 32 of 128 208/596, 180/452.
 //   else as many pieces as there is room for, down to one chunk: a second round of
 //   workgroups costs more than longer pieces (64 pairs x 64 chunks of 128, forward with 512
-//   workgroups 94, with 1024 113; backward with 256 335, with 512 346).
+//   workgroups 94, with 1024 113; backward with 256 335, with 512 346).  The bf16 backward
+//   of head sizes up to 32 has a third round of 256 all the same: 192 pairs x 13 chunks
+//   take 68 us with 768 workgroups, 80 with 512 and 65 with 1024; 32 pairs x 64 52, 52, 59.
 // A backward's piece is a whole number of the forward's pieces: it starts from the
 // states that the forward left (the number above, or for packed ones the nearest).
 int64_t piece_chunks(const Lin* p, bool bwd) {

@@ -4,7 +4,7 @@
 // It is native because the host's time bounds these operators' small calls and
 // most training steps: an autograd node written in Python runs its backward on
 // the engine's thread, where taking the interpreter over costs more than the kernels
-// (a training step of a 14 x 14 stage: 185 us so, 38 us of them on the device; 82 to 100
+// (a training step of a 14 x 14 stage: 185 us so, 36 us of them on the device; 82 to 100
 // natively).
 #include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
